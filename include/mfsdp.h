@@ -10,6 +10,8 @@
  *   mfsdp_muon_step      -- Muon over a heterogeneous list of whole matrices the rank owns
  *   mfsdp_newton_schulz  -- the Newton-Schulz orthogonalisation of one matrix
  *   mfsdp_adamw_step     -- AdamW over the rank's tail tensors
+ *   mfsdp_linear_xent, mfsdp_linear_distill -- losses over a vocabulary with the gradients of the hidden states and of
+ *                           the output head
  *
  * Muon, per owned matrix with stored shape m x n (Section 5.1 uses torch.optim.Muon's update):
  *   buf <- buf + (1 - beta) (g - buf)                    momentum EMA
@@ -399,6 +401,78 @@ size_t mfsdp_orthonormal_factor_workspace_size(int64_t d);
  * stream, workspace and error rules as mfsdp_soap_step. */
 int mfsdp_orthonormal_factor(const float* a, float* q, int64_t d, void* workspace,
                              size_t workspace_bytes, void* stream);
+
+/* ---- Losses over a vocabulary (what makes the gradient of an output head) --------------------- */
+
+/* How the tokens' losses are put together: loss = scale / D sum_r a_r l_r with the token weights a_r; D = 1 (SUM) or the
+ * sum of a_r over the tokens that count (MEAN; where that is 0, the loss and every gradient are 0). */
+typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
+
+/* Most teacher logits per token of mfsdp_linear_distill. */
+#define MFSDP_MAX_TOP_LOGITS 256
+
+/* n tokens with hidden states x through an output head w: logits z = x w^T (n x v), which are never held as a whole (a
+ * chunk of rows at 16 bits each where gradients are asked for, none otherwise).
+ *   x, w         n x h and v x h of dtype (F32 or BF16), read only; 0 <= n <= 2^28, 1 <= v, h <= 2^20
+ *   reduction, scale  an mfsdp_reduction and a finite factor; the gradients are those of loss
+ *   token_weight optional n fp32 weights a_r (NULL: 1)
+ *   loss         optional, 1 fp32: the reduced loss
+ *   token_loss   optional, n fp32: l_r (neither weighted nor scaled; 0 for a token that does not count)
+ *   lse          optional, n fp32: log sum_v exp z_rv of the (tempered) logits; 0 for a token that does not count
+ *   dx, dw       optional, n x h and v x h of dtype: gradients of loss, overwritten (at least one of the five
+ *                outputs has to be given)
+ *   chunk_rows   0, or the most rows of x per pass where gradients are asked for (rounded up to 256): fewer rows take
+ *                less workspace and more time. 0: as many as fit 2 GiB of 16-bit logits.
+ * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0.
+ * Precision: bf16 products have fp32 accumulation; the softmax is formed in fp32, the sum of a row without its largest
+ * term, so that the loss of a token that the model is sure of keeps its digits; the logits' gradient is rounded to bf16
+ * before its two products, and each result once to bf16. F32: products at fp32 accuracy (three bf16 parts per operand),
+ * everything else in fp32. */
+typedef struct {
+  const void* x;
+  const void* w;
+  int64_t n;
+  int64_t v;
+  int64_t h;
+  int32_t dtype;
+  int32_t reduction;
+  double scale;
+  const float* token_weight;
+  float* loss;
+  float* token_loss;
+  float* lse;
+  void* dx;
+  void* dw;
+  int64_t chunk_rows;
+} mfsdp_head_loss;
+
+/* Bytes of device workspace for mfsdp_linear_xent (k = 1) and mfsdp_linear_distill with these arguments: copies of w (and
+ * of w^T for dx), the chunk's logits and their transpose, and for n beyond one chunk an fp32 sum of dw. Of the pointers
+ * only whether dx and dw are NULL is looked at. 0 on invalid arguments. */
+size_t mfsdp_head_loss_workspace_size(const mfsdp_head_loss* args, int32_t k);
+
+/* Softmax cross entropy with hard labels: l_r = lse_r - z_{r, t_r} + z_loss lse_r^2.
+ *   targets      n labels t_r, int32 (target_bytes 4) or int64 (8). A token with t_r = ignore_index does not count;
+ *                any other label outside [0, v) makes its l_r, and with it loss and gradients, NaN.
+ *   z_loss       >= 0
+ * Enqueued on `stream`, with no host synchronisation and no allocation. The workspace (device, 256-byte aligned, >= the
+ * size query) must not be in use by another call still running. Returns MFSDP_OK, MFSDP_E_INVALID, MFSDP_E_WORKSPACE or
+ * MFSDP_E_HIP; on an argument error nothing is enqueued. n = 0 gives loss 0 and dw 0. */
+int mfsdp_linear_xent(const mfsdp_head_loss* args, const void* targets, int32_t target_bytes, int64_t ignore_index,
+                      double z_loss, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's top logits: with q_r the softmax of the token's k teacher logits / temperature (over its
+ * filled slots) and p_r the softmax of z_r / temperature over the whole vocabulary,
+ *   l_r = KL(q_r || p_r) = sum_j q_rj (log q_rj - log p_{r, id_rj}).
+ *   ids          n x k vocabulary ids, int32 (id_bytes 4) or int64 (8), in any order; a negative one marks an empty slot,
+ *                one >= v makes l_r NaN; an id that fills several slots takes the sum of their q. A token without a
+ *                filled slot does not count.
+ *   logits       n x k teacher logits of logit_dtype (-inf: q = 0); those of empty slots are not looked at
+ *   k            1 .. MFSDP_MAX_TOP_LOGITS;  temperature > 0 (l_r is not multiplied by temperature^2: use scale)
+ * Everything else as mfsdp_linear_xent. */
+int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t id_bytes, const void* logits,
+                         int32_t logit_dtype, int32_t k, double temperature, void* workspace, size_t workspace_bytes,
+                         void* stream);
 
 /* ---- Owner planning (host only; no GPU, no stream) ---------------------------------------- */
 

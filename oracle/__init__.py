@@ -21,8 +21,11 @@ Where the paper is silent, the readings used are the ones stated in each functio
   inverse fourth root, ``shampoo.py``) and SOAP (Adam in the eigenbasis of Shampoo's statistics,
   ``soap.py``) on the same whole matrices.
 
+Beside the paper's step stand the losses that make the gradient of an output head (``losses.py``).
+
 Parity status: every function here is pinned by tests in ``tests/test_oracle_pins.py``,
-``tests/test_planner_pins.py``, ``tests/test_shampoo_pins.py`` and ``tests/test_soap_pins.py``.
+``tests/test_planner_pins.py``, ``tests/test_shampoo_pins.py``, ``tests/test_soap_pins.py`` and
+``tests/test_loss_pins.py``.
 """
 from .muon import (  # noqa: F401
     bf16_widen,
@@ -40,3 +43,4 @@ from .adamw import adamw_step  # noqa: F401
 from . import planner  # noqa: F401
 from . import shampoo  # noqa: F401
 from . import soap  # noqa: F401
+from . import losses  # noqa: F401

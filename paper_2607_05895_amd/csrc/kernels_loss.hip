@@ -1,0 +1,810 @@
+// Losses over a vocabulary from hidden states and an output head, with both gradients, without the n x v logits
+// (loss_internal.h says what is held where).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+#include <utility>
+
+#include "loss_internal.h"
+
+namespace mfsdp {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// row-major tensors of any width: vectors at their elements' alignment
+typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+using gptr = __attribute__((address_space(1))) T*;
+template <typename T>
+using lptr = __attribute__((address_space(3))) T*;
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+
+template <typename F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kBKE = 32;          // K elements per stage
+constexpr int kRowB = kBKE * 2;   // bytes per staged row
+constexpr int kStages = 5;
+
+// Slot of 16-byte chunk c of row r in LDS: c ^ swz(r) (bank-conflict-free fragment reads).
+__device__ __forceinline__ int swz(int r) { return ((r >> 1 ^ r >> 3) & 1) | (((r >> 2) & 1) << 1); }
+#define LOSS_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | (((n) >> 4) << 14) | (7 << 4) | (0xF << 8))
+#define LOSS_WAIT_LGKM0() __builtin_amdgcn_s_waitcnt(0xF | (7 << 4) | (0 << 8) | (3 << 14))
+
+// NW waves, 2 x NW/2, on a TB x TB tile; a wave's part is MI x 2 blocks of 32 x 32.
+template <int NW, int TB>
+struct Grid {
+  static constexpr int WN = NW / 2;
+  static constexpr int MI = TB / 64, NI = 2;
+  static_assert(WN * 64 == TB, "64 columns a wave");
+  static constexpr int STAGE = 2 * TB * kRowB;
+  static constexpr int DW = NW == 8 ? 4 : NW;             // waves that issue the loads
+  static constexpr int PL = TB / kBlkRows / DW;           // loads of P (and of Q) per issuing wave and step
+  static constexpr int DLOADS = 2 * PL;
+  static constexpr int SLOTS = (TB == kLossTile ? 1 : 2) * kGemmSlots;  // workgroups per XCD
+  static constexpr int BAND = TB == kLossTile ? 4 : 8;    // block rows of a locality band
+};
+
+struct Item {
+  int bi, bj, k0, nk;
+};
+
+// C = P Q^T on a persistent grid. The main loop is the one of the Newton-Schulz products: a five-stage LDS ring filled by
+// direct global->LDS loads of whole 1 KiB blocks, one barrier per K step of 32 between its two 16-wide slices, the next
+// step's fragments read while the second slice multiplies, and the next tile's first loads issued before this tile's
+// epilogue. Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
+// column); the order is arithmetic, so a launch needs no schedule in memory.
+template <int NW, int TB, int NSEG, int KIND>
+__global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm a) {
+  using G = Grid<NW, TB>;
+  constexpr int MI = G::MI, NI = G::NI, STAGE = G::STAGE, DW = G::DW, PL = G::PL, DLOADS = G::DLOADS;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * STAGE];
+
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int wm = w / G::WN, wn = w % G::WN;
+  const int xcd = blockIdx.x % kGemmXcds, slot = blockIdx.x / kGemmXcds;
+  const int tiles = a.tm * a.tn, total = tiles * a.splits;
+  const int per = min(G::SLOTS, (total + kGemmXcds - 1) / kGemmXcds);  // tiles of one group
+  if (slot >= per) return;
+  const int steps = NSEG * a.nk;
+
+  auto item_at = [&](int g, Item& it) -> bool {
+    const int i = g * per + slot;
+    if (i >= total) return false;
+    const int s = i / tiles, j = i - s * tiles;
+    const int band = j / (G::BAND * a.tn), r0 = band * G::BAND, hb = min(G::BAND, a.tm - r0);
+    const int jj = j - r0 * a.tn;
+    it.bj = jj / hb;
+    it.bi = r0 + jj - it.bj * hb;
+    it.k0 = s * a.kper;
+    it.nk = min(a.kper, steps - it.k0);
+    return true;
+  };
+
+  const bool issuer = w < DW;
+  const int drow = (w % DW) * 16 + (lane >> 2);
+  const int dchunk = (lane & 3) ^ swz(lane >> 2);
+  const int dma_off = (w % DW) * 1024;
+  const int64_t pstep = int64_t(DW * kBlkRows) * a.ldp, qstep = int64_t(DW * kBlkRows) * a.ldq;
+  const uint16_t *psrc = nullptr, *qsrc = nullptr;  // of the tile whose loads are being issued
+  auto aim = [&](const Item& it) {
+    psrc = a.P + blk_index(int64_t(it.bi) * TB + drow, dchunk * 8, a.ldp);
+    qsrc = a.Q + blk_index(int64_t(it.bj) * TB + drow, dchunk * 8, a.ldq);
+  };
+  auto issue = [&](int k, int stage) {  // k: step of all segments
+    int64_t po, qo;
+    if constexpr (NSEG == 1) {
+      po = qo = int64_t(k) * (kBlkRows * kBKE);
+    } else {
+      const int sg = k / a.nk, kk = k - sg * a.nk;
+      po = a.pseg[sg] + int64_t(kk) * (kBlkRows * kBKE);
+      qo = a.qseg[sg] + int64_t(kk) * (kBlkRows * kBKE);
+    }
+    lds_byte* sb = (lds_byte*)(smem + stage * STAGE + dma_off);
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+      __builtin_amdgcn_global_load_lds(psrc + i * pstep + po, sb + i * DW * 1024, 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+      __builtin_amdgcn_global_load_lds(qsrc + i * qstep + qo, sb + TB * kRowB + i * DW * 1024, 16, 0, 0);
+  };
+  // the first steps of a tile (past its end: its last step again, into stages nobody reads)
+  auto prologue = [&](const Item& it) {
+    aim(it);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) issue(it.k0 + min(s, it.nk - 1), s);
+  };
+
+  const int frow = lane & 31, fhalf = lane >> 5;
+  const int pbase = (wm * (MI * 32) + frow) * kRowB;
+  const int qbase = (TB + wn * (NI * 32) + frow) * kRowB;
+  const int slot0 = ((0 + fhalf) ^ swz(frow)) * 16;
+  const int slot1 = ((2 + fhalf) ^ swz(frow)) * 16;
+  constexpr int NMF = MI * NI, NRD = MI + NI;
+
+  int g = xcd;
+  Item cur, nxt;
+  if (!item_at(g, cur)) return;
+  if (issuer) prologue(cur);
+  while (true) {
+    g += kGemmXcds;
+    const bool has_next = item_at(g, nxt);
+
+    f32x16_t acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+    bf16x8_t pf0[MI], qf0[NI], pf1[MI], qf1[NI];
+    auto read_frags = [&](const uint8_t* sb, int sl, bf16x8_t* pf, bf16x8_t* qf) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) pf[i] = *reinterpret_cast<const bf16x8_t*>(sb + pbase + i * 32 * kRowB + sl);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) qf[j] = *reinterpret_cast<const bf16x8_t*>(sb + qbase + j * 32 * kRowB + sl);
+    };
+    auto mfma_slice = [&](const bf16x8_t* pf, const bf16x8_t* qf) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], pf[i], acc[i][j], 0, 0, 0);
+    };
+    auto main_loop = [&](auto issue_c) {
+      constexpr bool ISS = decltype(issue_c)::value;
+      constexpr int L = ISS ? DLOADS : 0;
+      const int nk = cur.nk, last = cur.k0 + nk - 1;
+      if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 2) * DLOADS);
+      __builtin_amdgcn_s_barrier();
+      read_frags(smem, slot0, pf0, qf0);
+      int cs = 0, ns = 1, fs = kStages - 1;
+      for (int kt = 0; kt < nk; ++kt) {
+        read_frags(smem + cs * STAGE, slot1, pf1, qf1);
+        mfma_slice(pf0, qf0);
+        static_assert(NMF >= DLOADS / (NW == 8 ? 1 : 2), "slice schedule");
+#pragma unroll
+        for (int i = 0; i < NMF; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // 1 MFMA
+          if (i < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // 1 LDS read
+        }
+        if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 3) * DLOADS);  // step kt + 1 has landed
+        __builtin_amdgcn_s_barrier();
+        if constexpr (ISS) issue(min(cur.k0 + kt + kStages - 1, last), fs);
+        read_frags(smem + ns * STAGE, slot0, pf0, qf0);
+        mfma_slice(pf1, qf1);
+#pragma unroll
+        for (int i = 0; i < NMF; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (i < L) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // 1 load
+          if (i < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        cs = ns;
+        ns = (ns + 1 == kStages) ? 0 : ns + 1;
+        fs = (fs + 1 == kStages) ? 0 : fs + 1;
+      }
+    };
+    if (issuer)
+      main_loop(std::true_type{});
+    else
+      main_loop(std::false_type{});
+    // this tile's last loads have landed and its fragments are read before the next tile's loads reuse the stages
+    LOSS_WAIT_VMCNT(0);
+    __builtin_amdgcn_s_barrier();
+    if (has_next && issuer) prologue(nxt);  // (leaves stage kStages - 1 to the epilogue)
+
+    // acc[mi][ni][4 gg + t] of a lane is element (row, column) of the wave's part with row = 32 mi + lane % 32,
+    // column = 32 ni + 8 gg + 4 (lane / 32) + t.
+    lds_byte* slab = (lds_byte*)(smem + (kStages - 1) * STAGE);
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // lane-dependent offsets are formed here, not kept through the main loop
+    const int er = ln & 31, eh = ln >> 5;
+    if constexpr (KIND == kLossLogits) {
+      const int c0 = cur.bj * TB + wn * 64;       // the wave's first column
+      const int left = a.cols - c0;               // real columns from there
+      const int wsw = swz((wm * 32 + er) & 15);
+      auto slab_off = [](int sr, int c) -> int {
+        return (((sr >> 4) * (TB / 32) + (c >> 5)) << 10) + ((sr & 15) << 6) + ((((c & 31) >> 3) ^ swz(sr & 15)) << 4) +
+               ((c & 7) << 1);
+      };
+      const int wr_base = slab_off(wm * 32 + er, wn * 64 + eh * 4);
+      static_for<MI>([&](auto mi_c) {
+        constexpr int mi = decltype(mi_c)::value;
+        const int row = cur.bi * TB + wm * (MI * 32) + mi * 32 + er;
+        float u[32];
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          u[e] = acc[mi][e >> 4][e & 15] * a.inv_t;
+          if (left < 64 && (e >> 4) * 32 + ((e & 15) >> 2) * 8 + eh * 4 + (e & 3) >= left) u[e] = -__builtin_inff();
+          m = fmaxf(m, u[e]);
+        }
+        m = fmaxf(m, __shfl_xor(m, 32));
+        // sum of the others' exp: the largest term itself is 1, and what is far below it must not vanish in that 1
+        float s = 0.0f, ones = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const bool top = u[e] == m;
+          const float x = __builtin_amdgcn_exp2f((u[e] - m) * kLog2e);
+          s += top ? 0.0f : x;
+          ones += top ? 1.0f : 0.0f;
+        }
+        s += __shfl_xor(s, 32);
+        ones += __shfl_xor(ones, 32);
+        if (left > 0 && eh == 0) {
+          const int64_t at = int64_t(c0 >> 6) * a.ldr + row;
+          a.gm[at] = m;
+          a.gs[at] = s + (ones - 1.0f);
+        }
+        for (int j = 0; j < a.k; ++j) {
+          const int id = a.ids[int64_t(row) * a.k + j] - c0;
+          if (id >= 0 && id < 64 && ((id >> 2) & 1) == eh) {
+            const int e = (id >> 5) * 16 + ((id >> 3) & 3) * 4 + (id & 3);
+            float z = 0.0f;
+#pragma unroll
+            for (int f = 0; f < 32; ++f) z = e == f ? u[f] : z;
+            a.zt[int64_t(row) * a.k + j] = z;
+          }
+        }
+        if (a.logits) {
+          float* dst = a.logits + int64_t(row) * a.ldc + c0;
+#pragma unroll
+          for (int p = 0; p < 8; ++p)
+            *(gptr<f32x4_t>)(dst + (p >> 2) * 32 + (p & 3) * 8 + eh * 4) =
+                f32x4_t{u[4 * p], u[4 * p + 1], u[4 * p + 2], u[4 * p + 3]};
+        }
+        if (a.codes) {
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            uint32_t q[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              q[t] = uint32_t(__builtin_rintf(fminf((m - u[4 * p + t]) * (kLossCodeStep * kLog2e), 65535.0f)));
+            *(lptr<u32x2>)(slab + wr_base + (p >> 2) * 1024 + ((((p & 3) ^ wsw) - wsw) << 4)) =
+                u32x2{q[0] | q[1] << 16, q[2] | q[3] << 16};
+          }
+          LOSS_WAIT_LGKM0();
+          __builtin_amdgcn_s_barrier();
+          const int rin = ln >> 2, ch = ln & 3;
+#pragma unroll
+          for (int b = 0; b < 4 * (TB / 32) / NW; ++b) {
+            const int blk = w * (4 * (TB / 32) / NW) + b, sp = blk / (TB / 32), cb = blk % (TB / 32);
+            const u32x4 val = *(lptr<u32x4>)(slab + (blk << 10) + (rin << 6) + ((ch ^ swz(rin)) << 4));
+            const int dr = (sp >> 1) * (MI * 32) + mi * 32 + (sp & 1) * 16 + rin;
+            *(gptr<u32x4>)(a.codes + blk_index(int64_t(cur.bi) * TB + dr, int64_t(cur.bj) * TB + cb * 32 + ch * 8, a.ldc)) = val;
+          }
+          __builtin_amdgcn_s_barrier();
+        }
+      });
+    } else {
+      const int i = (cur.bj * a.tm + cur.bi) * a.splits + cur.k0 / a.kper;  // tile and range
+      const int64_t tile_at = int64_t(i) * (TB * TB) + (w * MI * NI * 4 * 64 + ln) * 4;
+      if (a.prev) {
+#pragma unroll
+        for (int q = 0; q < MI * NI * 4; ++q) {
+          const f32x4_t p = *(gptr<const f32x4_t>)(a.prev + tile_at + q * 256);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) acc[q / (NI * 4)][(q >> 2) & 1][4 * (q & 3) + t] += p[t];
+        }
+      }
+      if (a.part) {
+#pragma unroll
+        for (int q = 0; q < MI * NI * 4; ++q) {
+          const f32x16_t& c = acc[q / (NI * 4)][(q >> 2) & 1];
+          *(gptr<f32x4_t>)(a.part + tile_at + q * 256) =
+              f32x4_t{c[4 * (q & 3)], c[4 * (q & 3) + 1], c[4 * (q & 3) + 2], c[4 * (q & 3) + 3]};
+        }
+      } else if (!a.out_bf16) {
+        static_for<MI>([&](auto mi_c) {
+          constexpr int mi = decltype(mi_c)::value;
+          const int row = cur.bi * TB + wm * (MI * 32) + mi * 32 + er;
+          if (row < a.rows) {
+            float* dst = (float*)a.out + int64_t(row) * a.ldo;
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+              const int c = cur.bj * TB + wn * 64 + (p >> 2) * 32 + (p & 3) * 8 + eh * 4;
+              const f32x16_t& v = acc[mi][p >> 2];
+              const int o = 4 * (p & 3);
+              if (c + 4 <= a.cols) {
+                *(gptr<f32x4_a4>)(dst + c) = f32x4_a4{v[o], v[o + 1], v[o + 2], v[o + 3]};
+              } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                  if (c + t < a.cols) *(gptr<float>)(dst + c + t) = v[o + t];
+              }
+            }
+          }
+        });
+      } else {
+        // bf16, row-major, through the free stage: rounds of 32 rows of each wave row, whole row segments per store; 16-byte
+        // slots XORed by the row
+        constexpr int SL = TB / 8, ROWS = 64;
+        auto at = [](int r, int s) { return r * (TB * 2) + ((s ^ r) & (SL - 1)) * 16; };
+        static_for<MI>([&](auto mi_c) {
+          constexpr int mi = decltype(mi_c)::value;
+          const int sr = wm * 32 + er;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            const f32x16_t& v = acc[mi][p >> 2];
+            const int o = 4 * (p & 3);
+            *(lptr<u32x2>)(slab + at(sr, wn * 8 + (p >> 2) * 4 + (p & 3)) + eh * 8) =
+                u32x2{pack_bf16x2(v[o], v[o + 1]), pack_bf16x2(v[o + 2], v[o + 3])};
+          }
+          LOSS_WAIT_LGKM0();
+          __builtin_amdgcn_s_barrier();
+          constexpr int RPI = 64 / SL, IT = ROWS / NW / RPI;  // rows per wave instruction, instructions
+#pragma unroll
+          for (int it = 0; it < IT; ++it) {
+            const int r = w * (ROWS / NW) + it * RPI + ln / SL, s = ln % SL;
+            const u32x4 val = *(lptr<u32x4>)(slab + at(r, s));
+            const int row = cur.bi * TB + (r >> 5) * (MI * 32) + mi * 32 + (r & 31), c = cur.bj * TB + s * 8;
+            if (row < a.rows) {
+              uint16_t* dst = (uint16_t*)a.out + int64_t(row) * a.ldo + c;
+              if (c + 8 <= a.cols) {
+                *(gptr<u32x4_a2>)dst = val;
+              } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+                  if (c + t < a.cols) *(gptr<uint16_t>)(dst + t) = uint16_t(val[t >> 1] >> (16 * (t & 1)));
+              }
+            }
+          }
+          __builtin_amdgcn_s_barrier();
+        });
+      }
+    }
+    if (!has_next) break;
+    cur = nxt;
+  }
+  LOSS_WAIT_VMCNT(0);
+}
+
+// 32 rows x 256 columns of bf16 in LDS, as 16 x 32 blocks of swizzled 16-byte chunks; and one 16-byte piece of the
+// transposed block of columns 16 jp .. (lane: column lane % 16, rows 8 (lane / 16) ..).
+__device__ __forceinline__ int tile_off(int r, int c) {
+  return (((r >> 4) * 8 + (c >> 5)) << 10) + ((r & 15) << 6) + ((((c & 31) >> 3) ^ swz(r & 15)) << 4) + ((c & 7) << 1);
+}
+__device__ __forceinline__ u32x4 transposed_piece(lds_byte* tile, int jp, int ln) {
+  const int r = (ln >> 4) * 8 + ((ln >> 2) & 3), c = jp * 16 + (ln & 3) * 4;
+  const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)(tile + tile_off(r, c)));
+  const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)(tile + tile_off(r + 4, c)));
+  return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// the next of an fp32 value's three bf16 parts; what is left of the values stays in x
+__device__ __forceinline__ u32x4 split8(float (&x)[8]) {
+  u32x4 o;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    o[t] = pack_bf16x2(x[2 * t], x[2 * t + 1]);
+    x[2 * t] -= __uint_as_float(o[t] << 16);
+    x[2 * t + 1] -= __uint_as_float(o[t] & 0xffff0000u);
+  }
+  return o;
+}
+
+// One 32 x 256 tile per workgroup of 256: four 8-column chunks per thread (row it * 8 + t / 32, chunk t % 32).
+__global__ __launch_bounds__(256) void loss_pack_kernel(const LossPack2 b) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
+  lds_byte* tile = (lds_byte*)smem;
+  const LossPack& d = b.d[b.count > 1 && int(blockIdx.x) >= b.d[1].blocks_begin ? 1 : 0];
+  const int64_t i = int(blockIdx.x) - d.blocks_begin;
+  const int64_t tc = d.cols / 256, r0 = i / tc * 32, c0 = i % tc * 256;
+  const int t = threadIdx.x, ch = t & 31;
+  const int64_t c = c0 + ch * 8;
+  float x[4][8];
+#pragma unroll
+  for (int it = 0; it < 4; ++it) {
+    const int64_t r = r0 + it * 8 + (t >> 5);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[it][e] = 0.0f;
+    if (r < d.R && c < d.C && !(d.row_on && d.row_on[r] == 0.0f)) {
+      const int64_t at = r * d.C + c;
+      if (d.bf16) {
+        const uint16_t* p = (const uint16_t*)d.src + at;
+        if (c + 8 <= d.C) {
+          const u32x4_a2 v = *(gptr<const u32x4_a2>)p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[it][2 * e] = __uint_as_float(v[e] << 16);
+            x[it][2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e < d.C) x[it][e] = __uint_as_float(uint32_t(p[e]) << 16);
+        }
+      } else {
+        const float* p = (const float*)d.src + at;
+        if (c + 8 <= d.C) {
+          const f32x4_a4 v0 = *(gptr<const f32x4_a4>)p, v1 = *(gptr<const f32x4_a4>)(p + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[it][e] = v0[e];
+            x[it][4 + e] = v1[e];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e < d.C) x[it][e] = p[e];
+        }
+      }
+    }
+  }
+  const int ln = t & 63, w = t >> 6;
+  for (int part = 0; part < (d.bf16 ? 1 : 3); ++part) {
+    if (part) __syncthreads();  // the last part's transposed reads are done
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const u32x4 v = split8(x[it]);
+      const int r = it * 8 + (t >> 5);
+      if (d.dst && c < d.ldn) *(gptr<u32x4>)(d.dst + part * d.dst_part + blk_index(r0 + r, c, d.ldn)) = v;
+      if (d.dst_t) *(lptr<u32x4>)(tile + tile_off(r, ch * 8)) = v;
+    }
+    if (d.dst_t) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int jp = w * 4 + j;
+        *(gptr<u32x4>)(d.dst_t + part * d.dst_t_part + blk_index(c0 + jp * 16 + (ln & 15), r0 + (ln >> 4) * 8, d.ldt)) =
+            transposed_piece(tile, jp, ln);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// One wave per token, lanes over its slots.
+__global__ __launch_bounds__(256) void loss_targets_kernel(const LossTargets a) {
+  const int ln = threadIdx.x & 63;
+  const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r >= a.n_pad) return;
+  constexpr int PER = kLossMaxTop / 64;
+  float lg[PER], m = -__builtin_inff();
+  int id[PER];
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * 64 + ln;
+    id[i] = -1;
+    lg[i] = -__builtin_inff();
+    if (r < a.n && j < a.k) {
+      const int64_t at = r * a.k + j;
+      const int64_t v = a.id64 ? ((const int64_t*)a.ids)[at] : int64_t(((const int32_t*)a.ids)[at]);
+      const bool none = a.logits ? v < 0 : v == a.ignore;
+      if (!none) {
+        bad |= v < 0 || v >= a.v;
+        id[i] = v >= 0 && v < a.v ? int(v) : -1;
+        lg[i] = !a.logits ? 0.0f
+                : (a.logits_bf16 ? __uint_as_float(uint32_t(((const uint16_t*)a.logits)[at]) << 16)
+                                 : ((const float*)a.logits)[at]) * a.inv_t;
+        m = fmaxf(m, lg[i]);
+        if (!(lg[i] == lg[i])) bad = true;  // a NaN teacher logit
+      }
+    }
+  }
+  m = wave_max(m);
+  bad = __any(bad);
+  // (a row whose slots are all empty, or all of logit -inf, teaches nothing)
+  const bool on = m > -__builtin_inff();
+  float e[PER], s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    e[i] = on && lg[i] > -__builtin_inff() ? expf(lg[i] - m) : 0.0f;
+    s += e[i];
+  }
+  s = wave_sum(s);
+  float ent = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * 64 + ln;
+    const float q = on ? e[i] / s : 0.0f;
+    if (q > 0.0f) ent += q * ((lg[i] - m) - logf(s));
+    if (j < a.k) {
+      a.id[r * a.k + j] = on ? id[i] : -1;
+      a.q[r * a.k + j] = q;
+    }
+  }
+  ent = wave_sum(ent);
+  if (ln == 0) {
+    a.ent[r] = ent;
+    a.on[r] = bad ? __builtin_nanf("") : on ? 1.0f : 0.0f;
+  }
+}
+
+// One workgroup of 1024: a sum in a fixed order (64-bit, so that it does not depend on how many there are).
+__global__ __launch_bounds__(1024) void loss_sum_kernel(const float* a, const float* b, int64_t n, float scale,
+                                                        const float* denom, float* out) {
+  __shared__ double part[16];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 1024) s += b && a[i] != 0.0f ? double(a[i]) * b[i] : double(a[i]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int i = 0; i < 16; ++i) s += part[i];
+    s *= scale;
+    if (denom) s = denom[0] != 0.0f ? s / denom[0] : (s == s ? 0.0 : s);
+    out[0] = float(s);
+  }
+}
+
+// (m, s) of two sets joined: m the largest, s the sum of exp(. - m) over all others.
+__device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float s2) {
+  const float hi = fmaxf(m, m2), lo = fminf(m, m2);
+  const float sh = m >= m2 ? s : s2, sl = m >= m2 ? s2 : s;
+  s = lo > -__builtin_inff() ? sh + (sl + 1.0f) * __builtin_amdgcn_exp2f((lo - hi) * kLog2e) : sh + sl * 0.0f;
+  m = hi;
+}
+
+// 32 rows per workgroup of 1024: thread t goes through groups t / 32, + 32, ... of row t % 32.
+__global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
+  __shared__ float sm[32][33], ss[32][33];
+  const int rl = threadIdx.x & 31, gl = threadIdx.x >> 5;
+  const int64_t r = int64_t(blockIdx.x) * 32 + rl;
+  float m = -__builtin_inff(), s = 0.0f;
+  for (int g = gl; g < a.groups; g += 32) join_softmax(m, s, a.gm[g * a.ldr + r], a.gs[g * a.ldr + r]);
+  sm[gl][rl] = m;
+  ss[gl][rl] = s;
+  __syncthreads();
+  if (gl != 0) return;
+  for (int i = 1; i < 32; ++i) join_softmax(m, s, sm[i][rl], ss[i][rl]);
+  if (r >= a.rows) {
+    a.row[r] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+    return;
+  }
+  const float on = a.on[r];
+  const float ls = log1pf(s), lse = m + ls;
+  float loss = 0.0f;
+  if (on != 0.0f) {
+    float d = a.ent[r];
+    for (int j = 0; j < a.k; ++j) {
+      const float q = a.q[r * a.k + j];
+      if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (m - a.zt[r * a.k + j]);
+    }
+    loss = (d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
+  }
+  const float wt = on != 0.0f ? (a.weight ? a.weight[r] : 1.0f) : 0.0f;
+  float gf = a.scale * wt * on * a.inv_t;
+  if (on == 0.0f) gf = 0.0f;
+  else if (a.denom) gf = a.denom[0] != 0.0f ? gf / a.denom[0] : gf * 0.0f;
+  a.row[r] = float4{m, s, gf, 2.0f * a.z_loss * lse};
+  if (a.token_loss) a.token_loss[r] = loss;
+  if (a.lse) a.lse[r] = on != 0.0f ? lse : 0.0f;
+  a.weighted[r] = on != 0.0f ? wt * loss : 0.0f;
+}
+
+// One 32 x 256 tile of dz per workgroup of 256: from the logits to LDS, the targets' elements there from their fp32 logits,
+// then out in both layouts. Bound by HBM: 2 bytes read and 4 written per logit (bf16).
+template <bool F32>
+__global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
+  __shared__ float fix[F32 ? 32 * 256 : 1];
+  lds_byte* tile = (lds_byte*)smem;
+  const int tc = a.v_pad / 256;
+  const int64_t r0 = int64_t(blockIdx.x / tc) * 32, c0 = int64_t(blockIdx.x % tc) * 256;
+  const int t = threadIdx.x, ln = t & 63, w = t >> 6;
+  // chunk (row, 8 columns) it of a thread: bf16 as its 1 KiB block lies (lane: row lane / 4, chunk lane % 4); fp32
+  // along the row
+  auto crow = [&](int it) { return F32 ? it * 8 + (t >> 5) : (it >> 1) * 16 + (ln >> 2); };
+  auto ccol = [&](int it) { return F32 ? (t & 31) * 8 : (w * 2 + (it & 1)) * 32 + (ln & 3) * 8; };
+#pragma unroll
+  for (int it = 0; it < 4; ++it) {
+    const int r = crow(it), cl = ccol(it);
+    const int64_t row = r0 + r, c = c0 + cl;
+    const float4 rw = a.row[row];
+    const float f = rw.z * (1.0f + rw.w) / (1.0f + rw.y);
+    float x[8];
+    if constexpr (F32) {
+      const f32x4_t v0 = *(gptr<const f32x4_t>)(a.logits + row * a.ldc + c);
+      const f32x4_t v1 = *(gptr<const f32x4_t>)(a.logits + row * a.ldc + c + 4);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        x[e] = rw.z != 0.0f && c + e < a.v ? expf((e < 4 ? v0[e & 3] : v1[e & 3]) - rw.x) * f : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) fix[r * 256 + cl + e] = x[e];
+    } else {
+      const u32x4 v = *(gptr<const u32x4>)(a.codes + blk_index(row, c, a.ldc));
+      const float m = c < a.v ? a.gm[(c >> 6) * a.ldr + row] : 0.0f;
+      const float base = (m - rw.x) * kLog2e;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t q = v[e >> 1] >> (16 * (e & 1)) & 0xffff;
+        const float p = q == 65535u ? 0.0f : __builtin_amdgcn_exp2f(base - float(q) * (1.0f / kLossCodeStep));
+        x[e] = rw.z != 0.0f && c + e < a.v ? p * f : 0.0f;
+      }
+      *(lptr<u32x4>)(tile + tile_off(r, cl)) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                     pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+    }
+  }
+  __syncthreads();
+  for (int i = t; i < 32 * a.k; i += 256) {
+    const int r = i / a.k;
+    const int64_t row = r0 + r, at = row * a.k + (i - r * a.k);
+    const int id = a.id[at] - int(c0);
+    if (id < 0 || id >= 256 || a.id[at] < 0) continue;
+    const float4 rw = a.row[row];
+    if (rw.z == 0.0f) continue;
+    float q = 0.0f;  // of all slots with this id: each of them writes the same value
+    for (int j = 0; j < a.k; ++j) q += a.id[row * a.k + j] == a.id[at] ? a.q[row * a.k + j] : 0.0f;
+    const float d = a.zt[at] - rw.x, e = expf(d);
+    // p - q, from what is exact where both are near 1
+    const float pq = e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * rw.y : e - q * (1.0f + rw.y);
+    const float x = rw.z * (pq + rw.w * e) / (1.0f + rw.y);
+    if constexpr (F32)
+      fix[r * 256 + id] = x;
+    else
+      *(lptr<uint16_t>)(tile + tile_off(r, id)) = uint16_t(pack_bf16x2(x, 0.0f));
+  }
+  __syncthreads();
+  for (int part = 0; part < (F32 ? 3 : 1); ++part) {
+    if constexpr (F32) {
+      if (part) __syncthreads();
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int r = crow(it), cl = ccol(it);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fix[r * 256 + cl + e];
+        const u32x4 v = split8(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fix[r * 256 + cl + e] = x[e];
+        *(gptr<u32x4>)(a.dz + part * a.dz_part + blk_index(r0 + r, c0 + cl, a.ldc)) = v;
+        *(lptr<u32x4>)(tile + tile_off(r, cl)) = v;
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int it = 0; it < 4; ++it)
+        *(gptr<u32x4>)(a.dz + blk_index(r0 + crow(it), c0 + ccol(it), a.ldc)) = *(lptr<u32x4>)(tile + tile_off(crow(it), ccol(it)));
+    }
+    if (!a.dz_t) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int jp = w * 4 + j;
+      *(gptr<u32x4>)(a.dz_t + part * a.dz_t_part + blk_index(c0 + jp * 16 + (ln & 15), r0 + (ln >> 4) * 8, a.ldt)) =
+          transposed_piece(tile, jp, ln);
+    }
+  }
+}
+
+// The K ranges' partial tiles added in order; four elements per thread.
+template <int NW, int TB>
+__global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
+  using G = Grid<NW, TB>;
+  constexpr int Q = TB * TB / 4;
+  const int tile = blockIdx.x / (Q / 256), q = (blockIdx.x % (Q / 256)) * 256 + threadIdx.x;
+  const float* p = a.part + int64_t(tile) * a.splits * (TB * TB) + q * 4;
+  f32x4_t s = *(gptr<const f32x4_t>)p;
+  for (int i = 1; i < a.splits; ++i) s += *(gptr<const f32x4_t>)(p + int64_t(i) * (TB * TB));
+  const int ln = q & 63, blk = (q >> 6) & (G::MI * G::NI * 4 - 1), w = (q >> 6) / (G::MI * G::NI * 4);
+  const int bj = tile / a.tm, bi = tile - bj * a.tm;
+  const int row = bi * TB + (w / G::WN) * (G::MI * 32) + (blk >> 3) * 32 + (ln & 31);
+  const int c = bj * TB + (w % G::WN) * 64 + ((blk >> 2) & 1) * 32 + (blk & 3) * 8 + (ln >> 5) * 4;
+  if (row >= a.rows || c >= a.cols) return;
+  const int64_t at = int64_t(row) * a.ldo + c;
+  if (a.out_bf16) {
+    const u32x2 v = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+    uint16_t* o = (uint16_t*)a.out + at;
+    if (c + 4 <= a.cols) {
+      *(gptr<u32x2_a2>)o = v;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (c + t < a.cols) o[t] = uint16_t(v[t >> 1] >> (16 * (t & 1)));
+    }
+  } else {
+    float* o = (float*)a.out + at;
+    if (c + 4 <= a.cols) {
+      *(gptr<f32x4_a4>)o = s;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (c + t < a.cols) o[t] = s[t];
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void loss_zero_kernel(uint16_t* p, int64_t n) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) p[i] = 0;
+}
+
+template <int NW, int TB, int KIND>
+void launch_gemm_seg(const LossGemm& a, hipStream_t st) {
+  const dim3 grid(kGemmXcds * Grid<NW, TB>::SLOTS), block(NW * 64);
+  if (a.nseg == 1)
+    hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, 1, KIND>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, kLossMaxSeg, KIND>), grid, block, 0, st, a);
+}
+
+}  // namespace
+
+hipError_t launch_loss_gemm(const LossGemm& a, int kind, int tile, hipStream_t st) {
+  if (tile == kLossTile) {
+    if (kind == kLossLogits) launch_gemm_seg<8, kLossTile, kLossLogits>(a, st);
+    else launch_gemm_seg<8, kLossTile, kLossOut>(a, st);
+  } else {
+    if (kind == kLossLogits) launch_gemm_seg<4, kLossTileSmall, kLossLogits>(a, st);
+    else launch_gemm_seg<4, kLossTileSmall, kLossOut>(a, st);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_pack(const LossPack2& a, int blocks, hipStream_t st) {
+  hipLaunchKernelGGL(loss_pack_kernel, dim3(blocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_targets(const LossTargets& a, hipStream_t st) {
+  hipLaunchKernelGGL(loss_targets_kernel, dim3(unsigned((a.n_pad + 3) / 4)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_sum(const float* a, const float* b, int64_t n, float scale, const float* denom, float* out,
+                           hipStream_t st) {
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, a, b, n, scale, denom, out);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_rows(const LossRows& a, hipStream_t st) {
+  hipLaunchKernelGGL(loss_rows_kernel, dim3(a.rows_pad / 32), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st) {
+  const dim3 grid(unsigned(a.rows_pad / 32) * unsigned(a.v_pad / 256));
+  if (a.logits)
+    hipLaunchKernelGGL(loss_grad_kernel<true>, grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(loss_grad_kernel<false>, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st) {
+  const dim3 grid(unsigned(a.tiles) * unsigned(tile * tile / 1024));
+  if (tile == kLossTile)
+    hipLaunchKernelGGL((loss_join_kernel<8, kLossTile>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((loss_join_kernel<4, kLossTileSmall>), grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st) {
+  const int64_t n = bytes / 2;
+  if (n > 0) {
+    const int64_t g = (n + 255) / 256;
+    hipLaunchKernelGGL(loss_zero_kernel, dim3(unsigned(g < 4096 ? g : 4096)), dim3(256), 0, st, (uint16_t*)p, n);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mfsdp

@@ -1,0 +1,410 @@
+// Host side of the losses over a vocabulary: argument checks, workspace plan and launch sequence (all on the caller's
+// stream, descriptors as kernel arguments).
+//
+//   targets   ids, weights and entropy per token in one form; with MEAN the sum of the counted tokens' weights
+//   pack      x (this chunk's rows) and w as panel-blocked bf16, and transposed where a gradient reads them so
+//   per chunk of rows:
+//     logits  z = x w^T: per row and 64 columns the softmax partials, the targets' logits and (for gradients) the logits
+//     rows    the partials joined: loss, and the factor of the row's gradient
+//     grad    dz, in both layouts
+//     dx      dz w            (K ranges and their join where there are few tiles)
+//     dw      dz^T x          (added to the earlier chunks' sum, held in fp32)
+//   loss      the sum over the tokens
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "../../include/mfsdp.h"
+#include "loss_internal.h"
+
+using namespace mfsdp;
+
+namespace mfsdp {
+int set_last_error(int status, const std::string& msg);
+}
+
+namespace {
+
+static_assert(MFSDP_MAX_TOP_LOGITS == kLossMaxTop, "teacher logits of the ABI and the kernel");
+
+constexpr int64_t kMaxTokens = int64_t(1) << 28;
+constexpr int64_t kMaxSide = int64_t(1) << 20;
+constexpr int64_t kMaxChunk = 65536;
+constexpr int64_t kLogitBytes = int64_t(1) << 31;  // of a chunk's logits, at 16 bits each
+
+int fail(int status, const std::string& msg) { return set_last_error(status, msg); }
+int hip_fail(hipError_t e, const char* what) {
+  return fail(MFSDP_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+struct Gemm {
+  int tile = 0, tm = 0, tn = 0, splits = 1, kper = 0, nk = 0;
+};
+
+struct Plan {
+  bool f32 = false, grads = false;
+  int parts = 1, nseg = 1;
+  int64_t n = 0, v = 0, h = 0, k = 1;
+  int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0, groups = 0;
+  Gemm logits, dx, dw;
+  // offsets
+  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, row = 0, zt = 0, gm = 0, gs = 0;
+  size_t xb = 0, xt = 0, wb = 0, wt = 0, codes = 0, z32 = 0, dz_t = 0, part = 0, acc = 0;
+  size_t bytes = 0;
+};
+
+// Tile and K ranges of one product of M x N with K steps: the choice whose rounds of tiles over the chip's workgroups take
+// least, a step of a 256 x 256 tile taken as 1, of two 128 x 128 tiles on one CU as 0.6, a tile's start and epilogue as 12 steps and
+// the join of the ranges as its traffic.
+Gemm choose(int64_t M, int64_t N, int64_t steps, bool may_split) {
+  Gemm best;
+  double cost = 0.0;
+  for (int tile : {kLossTile, kLossTileSmall}) {
+    const int64_t tm = up(M, tile) / tile, tn = up(N, tile) / tile, tiles = tm * tn;
+    const int64_t slots = tile == kLossTile ? 256 : 512;
+    const int most = may_split ? int(std::max<int64_t>(1, std::min<int64_t>(16, steps / 16))) : 1;
+    for (int s = 1; s <= most; ++s) {
+      const int64_t kper = (steps + s - 1) / s;
+      if ((steps + kper - 1) / kper != s) continue;
+      // 128 x 128 tiles: one workgroup per CU while there are at most 256 of them (a step then takes 0.35)
+      const int64_t items = tiles * s;
+      const double per_step = tile == kLossTile ? 1.0 : items <= 256 ? 0.35 : 0.6;
+      const double rounds = double((items + slots - 1) / slots);
+      double c = rounds * (double(kper) + 12.0) * per_step;
+      if (s > 1) c += 8.0 + double(tiles) * s * tile * tile * 8.0 / 4.9e6;
+      if (best.tile == 0 || c < cost) {
+        cost = c;
+        best.tile = tile;
+        best.tm = int(tm);
+        best.tn = int(tn);
+        best.splits = s;
+        best.kper = int(kper);
+      }
+    }
+  }
+  return best;
+}
+
+int check(const mfsdp_head_loss* a, int64_t k, bool pointers) {
+  if (!a) return fail(MFSDP_E_INVALID, "arguments are NULL");
+  if (a->n < 0 || a->n > kMaxTokens) return fail(MFSDP_E_INVALID, "n must be in [0, 2^28]");
+  if (a->v < 1 || a->v > kMaxSide) return fail(MFSDP_E_INVALID, "v must be in [1, 2^20]");
+  if (a->h < 1 || a->h > kMaxSide) return fail(MFSDP_E_INVALID, "h must be in [1, 2^20]");
+  if (k < 1 || k > kLossMaxTop) return fail(MFSDP_E_INVALID, "k must be in [1, MFSDP_MAX_TOP_LOGITS]");
+  if (a->dtype != MFSDP_F32 && a->dtype != MFSDP_BF16) return fail(MFSDP_E_INVALID, "unsupported dtype");
+  if (a->reduction != MFSDP_SUM && a->reduction != MFSDP_MEAN) return fail(MFSDP_E_INVALID, "unknown reduction");
+  if (!std::isfinite(a->scale)) return fail(MFSDP_E_INVALID, "scale must be finite");
+  if (a->chunk_rows < 0) return fail(MFSDP_E_INVALID, "chunk_rows must be >= 0");
+  if (!pointers) return MFSDP_OK;
+  if (!a->w || (a->n > 0 && !a->x)) return fail(MFSDP_E_INVALID, "x or w is NULL");
+  if (!a->loss && !a->token_loss && !a->lse && !a->dx && !a->dw)
+    return fail(MFSDP_E_INVALID, "every output is NULL");
+  for (const void* p : {a->x, a->w, (const void*)a->token_weight, (const void*)a->loss, (const void*)a->token_loss,
+                        (const void*)a->lse, (const void*)a->dx, (const void*)a->dw})
+    if (!aligned16(p)) return fail(MFSDP_E_INVALID, "pointers must be 16-byte aligned");
+  return MFSDP_OK;
+}
+
+Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
+  Plan p;
+  p.f32 = a->dtype == MFSDP_F32;
+  p.grads = a->dx || a->dw;
+  p.parts = p.f32 ? 3 : 1;
+  p.nseg = p.f32 ? 6 : 1;
+  p.n = a->n;
+  p.v = a->v;
+  p.h = a->h;
+  p.k = k;
+  p.vp = up(p.v, 256);
+  p.hk = up(p.h, 32);
+  p.hp = up(p.h, 256);
+  p.groups = (p.v + kLossGroup - 1) / kLossGroup;
+  p.n_pad = up(std::max<int64_t>(p.n, 1), 256);
+  int64_t most = kMaxChunk;
+  if (p.grads) most = std::min(most, std::max<int64_t>(256, kLogitBytes / (2 * p.vp) / 256 * 256));
+  if (a->chunk_rows > 0) most = std::min(most, up(a->chunk_rows, 256));
+  p.chunk = std::min(p.n_pad, most);
+  p.logits = choose(p.chunk, p.v, p.nseg * p.hk / 32, false);
+  p.logits.nk = int(p.hk / 32);
+  const int64_t vsteps = up(p.v, 32) / 32;
+  if (a->dx) {
+    p.dx = choose(p.chunk, p.h, p.nseg * vsteps, true);
+    p.dx.nk = int(vsteps);
+  }
+  if (a->dw) p.dw = choose(p.v, p.h, p.nseg * p.chunk / 32, false);
+  size_t o = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t at = o;
+    o += size_t(up(bytes, 256));
+    return at;
+  };
+  const int64_t es = 2 * p.parts;
+  p.id = take(p.n_pad * k * 4);
+  p.q = take(p.n_pad * k * 4);
+  p.ent = take(p.n_pad * 4);
+  p.on = take(p.n_pad * 4);
+  p.weighted = take(p.n_pad * 4);
+  p.denom = take(4);
+  p.row = take(p.chunk * 16);
+  p.zt = take(p.chunk * k * 4);
+  p.gm = take((p.vp / kLossGroup) * p.chunk * 4);
+  p.gs = take((p.vp / kLossGroup) * p.chunk * 4);
+  p.xb = take(p.chunk * p.hk * es);
+  p.wb = take(p.vp * p.hk * es);
+  if (a->dw) p.xt = take(p.hp * p.chunk * es);
+  if (a->dx) p.wt = take(p.hp * p.vp * es);
+  if (p.grads) {
+    p.codes = take(p.chunk * p.vp * es);
+    if (p.f32) p.z32 = take(p.chunk * p.vp * 4);
+  }
+  if (a->dw) p.dz_t = take(p.vp * p.chunk * es);
+  if (p.dx.splits > 1) p.part = take(int64_t(p.dx.tm) * p.dx.tn * p.dx.splits * p.dx.tile * p.dx.tile * 4);
+  if (a->dw && p.chunk < p.n) p.acc = take(int64_t(p.dw.tm) * p.dw.tn * p.dw.tile * p.dw.tile * 4);
+  p.bytes = o;
+  return p;
+}
+
+struct Labels {
+  const void *ids, *logits;
+  int32_t id_bytes, logit_dtype;
+  int64_t ignore;
+  double temperature, z_loss;
+};
+
+int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, size_t workspace_bytes, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const int es = a->dtype == MFSDP_F32 ? 4 : 2;
+  const Plan p = make_plan(a, k);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return fail(MFSDP_E_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+  if (workspace_bytes < p.bytes)
+    return fail(MFSDP_E_WORKSPACE, "workspace too small: " + std::to_string(workspace_bytes) + " bytes, " +
+                                       std::to_string(p.bytes) + " needed");
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  auto f32p = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  auto u16p = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + off); };
+  hipError_t e;
+#define LOSS_TRY(call, what) \
+  if ((e = (call)) != hipSuccess) return hip_fail(e, what)
+
+  if (p.n == 0) {  // no token: loss 0, dw 0
+    if (a->loss) LOSS_TRY(launch_loss_zero(a->loss, 4, st), "zero launch");
+    if (a->dw) LOSS_TRY(launch_loss_zero(a->dw, p.v * p.h * es, st), "zero launch");
+    return MFSDP_OK;
+  }
+  const float inv_t = float(1.0 / l.temperature);
+  LossTargets t{};
+  t.ids = l.ids;
+  t.logits = l.logits;
+  t.id64 = l.id_bytes == 8;
+  t.logits_bf16 = l.logit_dtype == MFSDP_BF16;
+  t.k = int32_t(k);
+  t.n = p.n;
+  t.n_pad = p.n_pad;
+  t.v = p.v;
+  t.ignore = l.ignore;
+  t.inv_t = inv_t;
+  t.id = reinterpret_cast<int32_t*>(ws + p.id);
+  t.q = f32p(p.q);
+  t.ent = f32p(p.ent);
+  t.on = f32p(p.on);
+  LOSS_TRY(launch_loss_targets(t, st), "targets launch");
+  float* denom = nullptr;
+  if (a->reduction == MFSDP_MEAN) {
+    denom = f32p(p.denom);
+    LOSS_TRY(launch_loss_sum(t.on, a->token_weight, p.n, 1.0f, nullptr, denom, st), "weight sum launch");
+  }
+
+  const int64_t xpart = p.chunk * p.hk, xtpart = p.hp * p.chunk, wpart = p.vp * p.hk, wtpart = p.hp * p.vp;
+  const int64_t dzpart = p.chunk * p.vp;
+  // part pairs, the small products first: they are added while the sum is small
+  static const int kPair[kLossMaxSeg][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+  auto product = [&](const Gemm& g, size_t P, int64_t ldp, int64_t ppart, size_t Q, int64_t ldq, int64_t qpart, int nk) {
+    LossGemm m{};
+    m.P = u16p(P);
+    m.Q = u16p(Q);
+    m.ldp = ldp;
+    m.ldq = ldq;
+    m.nseg = p.nseg;
+    for (int s = 0; s < p.nseg && p.nseg > 1; ++s) {
+      m.pseg[s] = kPair[s][0] * ppart;
+      m.qseg[s] = kPair[s][1] * qpart;
+    }
+    m.nk = nk;
+    m.kper = g.splits > 1 ? g.kper : p.nseg * nk;
+    m.splits = (p.nseg * nk + m.kper - 1) / m.kper;
+    m.tm = g.tm;
+    m.tn = g.tn;
+    return m;
+  };
+  for (int64_t r0 = 0; r0 < p.n; r0 += p.chunk) {
+    const int64_t rows = std::min(p.chunk, p.n - r0), rows_pad = up(rows, 256);
+    LossPack2 pk{};
+    int blocks = 0;
+    auto pack = [&](const void* src, int64_t R, int64_t rpad, size_t dst, int64_t part, bool with_t, size_t dst_t,
+                    int64_t ldt, int64_t tpart, const float* on) {
+      LossPack& d = pk.d[pk.count++];
+      d.src = src;
+      d.R = R;
+      d.C = p.h;
+      d.dst = u16p(dst);
+      d.ldn = p.hk;
+      d.dst_part = part;
+      d.dst_t = with_t ? u16p(dst_t) : nullptr;
+      d.ldt = ldt;
+      d.dst_t_part = tpart;
+      d.rows = rpad;
+      d.cols = p.hp;
+      d.row_on = on;
+      d.blocks_begin = blocks;
+      d.bf16 = !p.f32;
+      blocks += int(rpad / 32 * (p.hp / 256));
+    };
+    pack(static_cast<const uint8_t*>(a->x) + r0 * p.h * es, rows, rows_pad, p.xb, xpart, a->dw != nullptr, p.xt, p.chunk,
+         xtpart, t.on + r0);
+    if (r0 == 0) pack(a->w, p.v, p.vp, p.wb, wpart, a->dx != nullptr, p.wt, p.vp, wtpart, nullptr);
+    LOSS_TRY(launch_loss_pack(pk, blocks, st), "pack launch");
+
+    LossGemm z = product(p.logits, p.xb, p.hk, xpart, p.wb, p.hk, wpart, p.logits.nk);
+    z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
+    z.rows = int(rows);
+    z.cols = int(p.v);
+    z.inv_t = inv_t;
+    z.gm = f32p(p.gm);
+    z.gs = f32p(p.gs);
+    z.ldr = p.chunk;
+    z.ids = t.id + r0 * k;
+    z.zt = f32p(p.zt);
+    z.k = int32_t(k);
+    z.ldc = p.vp;
+    if (p.grads && p.f32) z.logits = f32p(p.z32);
+    if (p.grads && !p.f32) z.codes = u16p(p.codes);
+    LOSS_TRY(launch_loss_gemm(z, kLossLogits, p.logits.tile, st), "logits launch");
+
+    LossRows rw{};
+    rw.gm = z.gm;
+    rw.gs = z.gs;
+    rw.ldr = p.chunk;
+    rw.groups = int(p.groups);
+    rw.rows = int(rows);
+    rw.rows_pad = int(rows_pad);
+    rw.k = int32_t(k);
+    rw.id = z.ids;
+    rw.q = t.q + r0 * k;
+    rw.ent = t.ent + r0;
+    rw.on = t.on + r0;
+    rw.weight = a->token_weight ? a->token_weight + r0 : nullptr;
+    rw.zt = z.zt;
+    rw.denom = denom;
+    rw.scale = float(a->scale);
+    rw.inv_t = inv_t;
+    rw.z_loss = float(l.z_loss);
+    rw.row = reinterpret_cast<float4*>(ws + p.row);
+    rw.token_loss = a->token_loss ? a->token_loss + r0 : nullptr;
+    rw.lse = a->lse ? a->lse + r0 : nullptr;
+    rw.weighted = f32p(p.weighted) + r0;
+    LOSS_TRY(launch_loss_rows(rw, st), "rows launch");
+    if (!p.grads) continue;
+
+    LossGrad gr{};
+    gr.codes = z.codes;
+    gr.logits = z.logits;
+    gr.ldc = p.vp;
+    gr.dz = u16p(p.codes);
+    gr.dz_t = a->dw ? u16p(p.dz_t) : nullptr;
+    gr.dz_part = dzpart;
+    gr.dz_t_part = dzpart;
+    gr.ldt = p.chunk;
+    gr.gm = z.gm;
+    gr.ldr = p.chunk;
+    gr.row = rw.row;
+    gr.id = z.ids;
+    gr.q = rw.q;
+    gr.zt = z.zt;
+    gr.k = int32_t(k);
+    gr.rows = int(rows);
+    gr.rows_pad = int(rows_pad);
+    gr.v = int(p.v);
+    gr.v_pad = int(p.vp);
+    LOSS_TRY(launch_loss_grad(gr, st), "gradient launch");
+
+    if (a->dx) {
+      LossGemm m = product(p.dx, p.codes, p.vp, dzpart, p.wt, p.vp, wtpart, p.dx.nk);
+      m.tm = int(up(rows, p.dx.tile) / p.dx.tile);
+      m.rows = int(rows);
+      m.cols = int(p.h);
+      m.out = static_cast<uint8_t*>(a->dx) + r0 * p.h * es;
+      m.ldo = p.h;
+      m.out_bf16 = !p.f32;
+      if (m.splits > 1) m.part = f32p(p.part);
+      LOSS_TRY(launch_loss_gemm(m, kLossOut, p.dx.tile, st), "dx launch");
+      if (m.splits > 1) {
+        LossJoin j{};
+        j.part = m.part;
+        j.splits = m.splits;
+        j.tiles = m.tm * m.tn;
+        j.tm = m.tm;
+        j.tn = m.tn;
+        j.rows = m.rows;
+        j.cols = m.cols;
+        j.out_bf16 = m.out_bf16;
+        j.out = m.out;
+        j.ldo = m.ldo;
+        LOSS_TRY(launch_loss_join(j, p.dx.tile, st), "dx join launch");
+      }
+    }
+    if (a->dw) {
+      LossGemm m = product(p.dw, p.dz_t, p.chunk, dzpart, p.xt, p.chunk, xtpart, int(up(rows, 32) / 32));
+      m.rows = int(p.v);
+      m.cols = int(p.h);
+      m.out = a->dw;
+      m.ldo = p.h;
+      m.out_bf16 = !p.f32;
+      if (r0 > 0) m.prev = f32p(p.acc);
+      if (r0 + p.chunk < p.n) m.part = f32p(p.acc);
+      LOSS_TRY(launch_loss_gemm(m, kLossOut, p.dw.tile, st), "dw launch");
+    }
+  }
+  if (a->loss)
+    LOSS_TRY(launch_loss_sum(f32p(p.weighted), nullptr, p.n, float(a->scale), denom, a->loss, st), "loss sum launch");
+#undef LOSS_TRY
+  return MFSDP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mfsdp_head_loss_workspace_size(const mfsdp_head_loss* args, int32_t k) {
+  if (check(args, k, false)) return 0;
+  return std::max<size_t>(make_plan(args, k).bytes, 256);
+}
+
+int mfsdp_linear_xent(const mfsdp_head_loss* args, const void* targets, int32_t target_bytes, int64_t ignore_index,
+                      double z_loss, void* workspace, size_t workspace_bytes, void* stream) {
+  if (const int rc = check(args, 1, true)) return rc;
+  if (!targets && args->n > 0) return fail(MFSDP_E_INVALID, "targets is NULL");
+  if (target_bytes != 4 && target_bytes != 8) return fail(MFSDP_E_INVALID, "target_bytes must be 4 or 8");
+  if (!aligned16(targets)) return fail(MFSDP_E_INVALID, "pointers must be 16-byte aligned");
+  if (!std::isfinite(z_loss) || z_loss < 0.0) return fail(MFSDP_E_INVALID, "z_loss must be >= 0");
+  return run(args, 1, Labels{targets, nullptr, target_bytes, 0, ignore_index, 1.0, z_loss}, workspace, workspace_bytes, stream);
+}
+
+int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t id_bytes, const void* logits,
+                         int32_t logit_dtype, int32_t k, double temperature, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (const int rc = check(args, k, true)) return rc;
+  if ((!ids || !logits) && args->n > 0) return fail(MFSDP_E_INVALID, "ids or logits is NULL");
+  if (id_bytes != 4 && id_bytes != 8) return fail(MFSDP_E_INVALID, "id_bytes must be 4 or 8");
+  if (logit_dtype != MFSDP_F32 && logit_dtype != MFSDP_BF16) return fail(MFSDP_E_INVALID, "unsupported logit dtype");
+  if (!aligned16(ids) || !aligned16(logits)) return fail(MFSDP_E_INVALID, "pointers must be 16-byte aligned");
+  if (!std::isfinite(temperature) || !(temperature > 0.0)) return fail(MFSDP_E_INVALID, "temperature must be > 0");
+  return run(args, k, Labels{ids, logits, id_bytes, logit_dtype, 0, temperature, 0.0}, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -24,7 +24,8 @@ EXPORTS = ("mfsdp_muon_workspace_size", "mfsdp_muon_step", "mfsdp_muon_step_time
            "mfsdp_shampoo_workspace_size", "mfsdp_shampoo_step", "mfsdp_inverse_root_workspace_size",
            "mfsdp_inverse_root", "mfsdp_soap_workspace_size", "mfsdp_soap_step",
            "mfsdp_orthonormal_factor_workspace_size", "mfsdp_orthonormal_factor", "mfsdp_build_id",
-           "mfsdp_muon_step_noalloc", "mfsdp_plan_layouts")
+           "mfsdp_muon_step_noalloc", "mfsdp_plan_layouts", "mfsdp_head_loss_workspace_size", "mfsdp_linear_xent",
+           "mfsdp_linear_distill")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 MAX_GRAD_PARTS = 64
 ABI_VERSION = 6
@@ -85,6 +86,18 @@ class SoapHParams(ctypes.Structure):
 class PlanParam(ctypes.Structure):
     _fields_ = [("block", ctypes.c_int32), ("is_matrix", ctypes.c_int32), ("numel", ctypes.c_int64)]
 
+
+class HeadLoss(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("n", ctypes.c_int64), ("v", ctypes.c_int64),
+                ("h", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reduction", ctypes.c_int32),
+                ("scale", ctypes.c_double), ("token_weight", ctypes.c_void_p), ("loss", ctypes.c_void_p),
+                ("token_loss", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("dw", ctypes.c_void_p), ("chunk_rows", ctypes.c_int64)]
+
+
+SUM, MEAN = 0, 1
+_REDUCTIONS = {"sum": SUM, "mean": MEAN}
+MAX_TOP_LOGITS = 256    # most teacher logits per token of mfsdp_linear_distill
 
 PLAN_ROLE_GREEDY, PLAN_SCOPE_GREEDY, PLAN_COST_AWARE = 0, 1, 2
 
@@ -164,6 +177,12 @@ def lib() -> ctypes.CDLL:
         L.mfsdp_orthonormal_factor_workspace_size.restype = sz
         L.mfsdp_orthonormal_factor.argtypes = [vp, vp, i64, vp, sz, vp]
         L.mfsdp_orthonormal_factor.restype = ctypes.c_int
+        L.mfsdp_head_loss_workspace_size.argtypes = [ctypes.POINTER(HeadLoss), i32]
+        L.mfsdp_head_loss_workspace_size.restype = sz
+        L.mfsdp_linear_xent.argtypes = [ctypes.POINTER(HeadLoss), vp, i32, i64, f64, vp, sz, vp]
+        L.mfsdp_linear_xent.restype = ctypes.c_int
+        L.mfsdp_linear_distill.argtypes = [ctypes.POINTER(HeadLoss), vp, i32, vp, i32, i32, f64, vp, sz, vp]
+        L.mfsdp_linear_distill.restype = ctypes.c_int
         L.mfsdp_build_id.argtypes = []
         L.mfsdp_build_id.restype = ctypes.c_char_p
         from . import build_lib
@@ -345,6 +364,25 @@ def mfsdp_adamw_step(entries: Sequence[AdamWEntry], lr: float, beta1: float, bet
                      eps: float, weight_decay: float, step: int, stream: int = 0) -> None:
     arr, n = _entries(entries, AdamWEntry)
     _check(lib().mfsdp_adamw_step(arr, n, lr, beta1, beta2, eps, weight_decay, step, stream))
+
+
+def mfsdp_head_loss_workspace_size(args: HeadLoss, k: int = 1) -> int:
+    size = lib().mfsdp_head_loss_workspace_size(ctypes.byref(args), k)
+    if size == 0:
+        raise MfsdpError(E_INVALID, mfsdp_last_error())
+    return size
+
+
+def mfsdp_linear_xent(args: HeadLoss, targets: int, target_bytes: int, ignore_index: int, z_loss: float,
+                      workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().mfsdp_linear_xent(ctypes.byref(args), targets, target_bytes, ignore_index, z_loss, workspace,
+                                   workspace_bytes, stream))
+
+
+def mfsdp_linear_distill(args: HeadLoss, ids: int, id_bytes: int, logits: int, logit_dtype: int, k: int,
+                         temperature: float, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().mfsdp_linear_distill(ctypes.byref(args), ids, id_bytes, logits, logit_dtype, k, temperature,
+                                      workspace, workspace_bytes, stream))
 
 
 # ------------------------------------------------------------------- torch tensor helpers
@@ -550,3 +588,56 @@ def orthonormal_factor_t(a, q, workspace=None) -> None:
                                 device=a.device)
     f = ("float32",)
     mfsdp_orthonormal_factor(_ptr(a, "a", (d, d), f), _ptr(q, "q", (d, d), f), d, *_ws(workspace), _stream())
+
+
+_INT = ("int64", "int32")
+
+
+def head_loss_args_t(x, w, loss=None, token_loss=None, lse=None, dx=None, dw=None, reduction="mean", scale=1.0,
+                     token_weight=None, chunk_rows=0) -> HeadLoss:
+    """The arguments that both losses share: hidden states x (n x h), head w (v x h), the outputs to write (any of them
+    None), the reduction ("mean" or "sum") and the scale of the loss."""
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise ValueError(f"x and w: (n, h) and (v, h) are required, got {tuple(x.shape)} and {tuple(w.shape)}")
+    n, h = x.shape
+    v = w.shape[0]
+    f, same = ("float32",), (str(x.dtype).replace("torch.", ""),)
+    opt = lambda t, what, shape, dts: _ptr(t, what, shape, dts) if t is not None else None  # noqa: E731
+    xp = _ptr(x, "x")
+    if loss is not None and loss.numel() != 1:
+        raise ValueError(f"loss: one element is required, got shape {tuple(loss.shape)}")
+    return HeadLoss(xp, _ptr(w, "w", (v, h), same), n, v, h, _dt(x),
+                    _REDUCTIONS[reduction] if isinstance(reduction, str) else int(reduction), float(scale),
+                    opt(token_weight, "token_weight", (n,), f), opt(loss, "loss", None, f),
+                    opt(token_loss, "token_loss", (n,), f), opt(lse, "lse", (n,), f), opt(dx, "dx", (n, h), same),
+                    opt(dw, "dw", (v, h), same), int(chunk_rows))
+
+
+def head_loss_workspace_t(args: HeadLoss, k: int = 1, device="cuda"):
+    import torch
+    return torch.empty(mfsdp_head_loss_workspace_size(args, k), dtype=torch.uint8, device=device)
+
+
+def linear_xent_t(x, w, targets, loss=None, token_loss=None, lse=None, dx=None, dw=None, ignore_index=-100,
+                  reduction="mean", scale=1.0, token_weight=None, z_loss=0.0, chunk_rows=0, workspace=None) -> None:
+    """Softmax cross entropy of x w^T with the labels `targets` (n, int64 or int32) into the outputs that are given, on
+    torch's current stream. workspace: head_loss_workspace_t's tensor (None: allocated for this call)."""
+    args = head_loss_args_t(x, w, loss, token_loss, lse, dx, dw, reduction, scale, token_weight, chunk_rows)
+    tp = _ptr(targets, "targets", (args.n,), _INT)
+    if workspace is None:
+        workspace = head_loss_workspace_t(args, 1, x.device)
+    mfsdp_linear_xent(args, tp, targets.element_size(), int(ignore_index), float(z_loss), *_ws(workspace), _stream())
+
+
+def linear_distill_t(x, w, ids, logits, loss=None, token_loss=None, lse=None, dx=None, dw=None, temperature=1.0,
+                     reduction="mean", scale=1.0, token_weight=None, chunk_rows=0, workspace=None) -> None:
+    """KL divergence from a teacher's top logits (`ids`, `logits`: n x k) to the softmax of x w^T / temperature, as
+    linear_xent_t."""
+    args = head_loss_args_t(x, w, loss, token_loss, lse, dx, dw, reduction, scale, token_weight, chunk_rows)
+    if ids.dim() != 2:
+        raise ValueError(f"ids: (n, k) is required, got shape {tuple(ids.shape)}")
+    k = ids.shape[1]
+    ip, lp = _ptr(ids, "ids", (args.n, k), _INT), _ptr(logits, "logits", (args.n, k))
+    if workspace is None:
+        workspace = head_loss_workspace_t(args, k, x.device)
+    mfsdp_linear_distill(args, ip, ids.element_size(), lp, _dt(logits), k, float(temperature), *_ws(workspace), _stream())

@@ -1,0 +1,104 @@
+"""Host-side tests of the losses over a vocabulary that need no GPU: refusals before anything is enqueued, and the size
+of the workspace."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2607_05895_amd import native
+
+FAKE = 1 << 20  # a 16-byte aligned non-NULL address; never dereferenced (validation fails first)
+
+
+def _args(**kw):
+    d = dict(x=FAKE, w=FAKE * 2, n=64, v=1000, h=128, dtype=native.BF16, reduction=native.MEAN, scale=1.0,
+             token_weight=None, loss=FAKE * 3, token_loss=None, lse=None, dx=FAKE * 4, dw=FAKE * 5, chunk_rows=0)
+    d.update(kw)
+    return native.HeadLoss(**d)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n=-1), dict(n=(1 << 28) + 1), dict(v=0), dict(v=(1 << 20) + 1), dict(h=0), dict(h=(1 << 20) + 1), dict(dtype=2),
+    dict(dtype=-1), dict(reduction=2), dict(scale=float("nan")), dict(scale=float("inf")), dict(chunk_rows=-1),
+])
+def test_bad_arguments_are_refused_by_every_entry(bad):
+    a = _args(**bad)
+    for call in (lambda: native.mfsdp_linear_xent(a, FAKE, 8, -100, 0.0, FAKE * 16, 1 << 50),
+                 lambda: native.mfsdp_linear_distill(a, FAKE, 8, FAKE, native.F32, 4, 1.0, FAKE * 16, 1 << 50),
+                 lambda: native.mfsdp_head_loss_workspace_size(a)):
+        with pytest.raises(native.MfsdpError) as ei:
+            call()
+        assert ei.value.status == native.E_INVALID
+
+
+@pytest.mark.parametrize("bad", [
+    dict(x=None), dict(w=None), dict(x=FAKE + 8), dict(w=FAKE + 2), dict(loss=FAKE + 4), dict(token_loss=FAKE + 4),
+    dict(lse=FAKE + 4), dict(dx=FAKE + 2), dict(dw=FAKE + 2), dict(token_weight=FAKE + 4),
+    dict(loss=None, dx=None, dw=None),
+])
+def test_bad_pointers_are_refused(bad):
+    a = _args(**bad)
+    for call in (lambda: native.mfsdp_linear_xent(a, FAKE, 8, -100, 0.0, FAKE * 16, 1 << 50),
+                 lambda: native.mfsdp_linear_distill(a, FAKE, 8, FAKE, native.F32, 4, 1.0, FAKE * 16, 1 << 50)):
+        with pytest.raises(native.MfsdpError) as ei:
+            call()
+        assert ei.value.status == native.E_INVALID
+
+
+@pytest.mark.parametrize("targets,size,z_loss", [(None, 8, 0.0), (FAKE + 8, 8, 0.0), (FAKE, 2, 0.0), (FAKE, 8, -1.0),
+                                                 (FAKE, 8, float("nan")), (FAKE, 8, float("inf"))])
+def test_bad_labels_are_refused(targets, size, z_loss):
+    with pytest.raises(native.MfsdpError) as ei:
+        native.mfsdp_linear_xent(_args(), targets, size, -100, z_loss, FAKE * 16, 1 << 50)
+    assert ei.value.status == native.E_INVALID
+
+
+@pytest.mark.parametrize("ids,size,logits,dt,k,temp", [
+    (None, 8, FAKE, 0, 4, 1.0), (FAKE, 8, None, 0, 4, 1.0), (FAKE, 1, FAKE, 0, 4, 1.0), (FAKE, 8, FAKE, 3, 4, 1.0),
+    (FAKE, 8, FAKE, 0, 0, 1.0), (FAKE, 8, FAKE, 0, 257, 1.0), (FAKE, 8, FAKE, 0, 4, 0.0), (FAKE, 8, FAKE, 0, 4, -1.0),
+    (FAKE, 8, FAKE, 0, 4, float("nan")), (FAKE, 8, FAKE, 0, 4, float("inf")), (FAKE + 4, 8, FAKE, 0, 4, 1.0),
+    (FAKE, 8, FAKE + 4, 0, 4, 1.0),
+])
+def test_bad_teachers_are_refused(ids, size, logits, dt, k, temp):
+    with pytest.raises(native.MfsdpError) as ei:
+        native.mfsdp_linear_distill(_args(), ids, size, logits, dt, k, temp, FAKE * 16, 1 << 50)
+    assert ei.value.status == native.E_INVALID
+
+
+@pytest.mark.parametrize("ws,bytes_", [(None, 1 << 50), (FAKE * 16 + 16, 1 << 50), (FAKE * 16, 1 << 10)])
+def test_bad_workspaces_are_refused(ws, bytes_):
+    for call in (lambda: native.mfsdp_linear_xent(_args(), FAKE, 8, -100, 0.0, ws, bytes_),
+                 lambda: native.mfsdp_linear_distill(_args(), FAKE, 8, FAKE, native.F32, 4, 1.0, ws, bytes_)):
+        with pytest.raises(native.MfsdpError) as ei:
+            call()
+        assert ei.value.status == native.E_WORKSPACE
+
+
+def test_null_arguments_are_refused():
+    assert native.lib().mfsdp_linear_xent(None, FAKE, 8, -100, 0.0, FAKE, 1 << 40, None) == native.E_INVALID
+    assert native.lib().mfsdp_head_loss_workspace_size(None, 1) == 0
+
+
+def test_workspace_does_not_hold_the_logits():
+    """128256 ids: beyond one chunk of rows the workspace grows by a few words per token, and without gradients it is
+    that of the packed operands."""
+    size = lambda **kw: native.mfsdp_head_loss_workspace_size(_args(v=128256, h=4096, **kw))  # noqa: E731
+    a, b = size(n=1 << 16), size(n=1 << 18)
+    assert (b - a) / ((1 << 18) - (1 << 16)) <= 32
+    assert a - size(n=1 << 16, chunk_rows=512) > 3.5 * (1 << 30)   # the chunk's logits and their transpose
+    assert size(n=1 << 16, dx=None, dw=None) < 3 * (1 << 30)
+    for n in (1, 255, 257):
+        assert size(n=n) < 4 * (1 << 30)
+
+
+def test_cpu_tensors_are_refused():
+    x, w, t = torch.zeros(4, 8), torch.zeros(16, 8), torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError, match="CUDA"):
+        native.linear_xent_t(x, w, t, loss=torch.zeros(1))
+    with pytest.raises(ValueError, match="CUDA"):
+        native.linear_distill_t(x, w, t[:, None], torch.zeros(4, 1), loss=torch.zeros(1))
+
+
+def test_struct_matches_the_header():
+    """8-byte fields and pairs of 4-byte ones: no padding anywhere."""
+    assert ctypes.sizeof(native.HeadLoss) == 8 * 14
