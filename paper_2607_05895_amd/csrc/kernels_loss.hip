@@ -60,14 +60,21 @@ struct Grid {
   static constexpr int BAND = TB == kLossTile ? 4 : 8;    // block rows of a locality band
 };
 
+// alpha / denom, 0 where denom is 0
+__device__ __forceinline__ float out_factor(float alpha, const float* denom) {
+  if (!denom) return alpha;
+  const float d = *denom;
+  return d != 0.0f ? alpha / d : 0.0f;
+}
+
 struct Item {
   int bi, bj, k0, nk;
 };
 
 // C = P Q^T on a persistent grid. The main loop is the one of the Newton-Schulz products: a five-stage LDS ring filled by
-// direct global->LDS loads of whole 1 KiB blocks, one barrier per K step of 32 between its two 16-wide slices, the next
-// step's fragments read while the second slice multiplies, and the next tile's first loads issued before this tile's
-// epilogue. Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
+// direct global->LDS loads of whole 1 KiB blocks by one wave of each SIMD, one barrier per K step of 32 inside its second
+// 16-wide slice, the next step's fragments read while the rest of that slice multiplies, and the next tile's first loads
+// issued before this tile's epilogue. Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
 // column); the order is arithmetic, so a launch needs no schedule in memory.
 template <int NW, int TB, int NSEG, int KIND>
 __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm a) {
@@ -75,7 +82,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   constexpr int MI = G::MI, NI = G::NI, STAGE = G::STAGE, DW = G::DW, PL = G::PL, DLOADS = G::DLOADS;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * STAGE];
 
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / G::WN, wn = w % G::WN;
   const int xcd = blockIdx.x % kGemmXcds, slot = blockIdx.x / kGemmXcds;
   const int tiles = a.tm * a.tn, total = tiles * a.splits;
@@ -97,37 +104,42 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   };
 
   const bool issuer = w < DW;
-  const int drow = (w % DW) * 16 + (lane >> 2);
-  const int dchunk = (lane & 3) ^ swz(lane >> 2);
-  const int dma_off = (w % DW) * 1024;
-  const int64_t pstep = int64_t(DW * kBlkRows) * a.ldp, qstep = int64_t(DW * kBlkRows) * a.ldq;
-  const uint16_t *psrc = nullptr, *qsrc = nullptr;  // of the tile whose loads are being issued
+  // load i of P (of Q) of issuing wave w moves the 1 KiB block of 16-row panel i DW + w: lane l its row l / 4, 16-byte chunk
+  // (l % 4) ^ swz(row), so that the fragment reads are conflict-free. One lane offset for all; the rest is scalar.
+  const uint32_t loff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
+  const uint32_t pstep = DW * kBlkRows * 2 * uint32_t(a.ldp), qstep = DW * kBlkRows * 2 * uint32_t(a.ldq);
+  const uint16_t *pbase_g = nullptr, *qbase_g = nullptr;  // the wave's first panels of the tile being loaded
+  __amdgpu_buffer_rsrc_t pr, qr;
+  auto rsrc = [](const uint16_t* p) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00020000); };
   auto aim = [&](const Item& it) {
-    psrc = a.P + blk_index(int64_t(it.bi) * TB + drow, dchunk * 8, a.ldp);
-    qsrc = a.Q + blk_index(int64_t(it.bj) * TB + drow, dchunk * 8, a.ldq);
-  };
-  auto issue = [&](int k, int stage) {  // k: step of all segments
-    int64_t po, qo;
+    pbase_g = a.P + (int64_t(it.bi) * TB + w * kBlkRows) * a.ldp;
+    qbase_g = a.Q + (int64_t(it.bj) * TB + w * kBlkRows) * a.ldq;
     if constexpr (NSEG == 1) {
-      po = qo = int64_t(k) * (kBlkRows * kBKE);
-    } else {
-      const int sg = k / a.nk, kk = k - sg * a.nk;
-      po = a.pseg[sg] + int64_t(kk) * (kBlkRows * kBKE);
-      qo = a.qseg[sg] + int64_t(kk) * (kBlkRows * kBKE);
+      pr = rsrc(pbase_g);
+      qr = rsrc(qbase_g);
     }
-    lds_byte* sb = (lds_byte*)(smem + stage * STAGE + dma_off);
-#pragma unroll
-    for (int i = 0; i < PL; ++i)
-      __builtin_amdgcn_global_load_lds(psrc + i * pstep + po, sb + i * DW * 1024, 16, 0, 0);
-#pragma unroll
-    for (int i = 0; i < PL; ++i)
-      __builtin_amdgcn_global_load_lds(qsrc + i * qstep + qo, sb + TB * kRowB + i * DW * 1024, 16, 0, 0);
+  };
+  // load l (0 .. PL - 1: of P, then of Q) of step k of all segments
+  auto issue = [&](int l, int k, int stage) {
+    int kk = k;
+    if constexpr (NSEG > 1) {
+      const int sg = k / a.nk;
+      kk = k - sg * a.nk;
+      if (l < PL) pr = rsrc(pbase_g + a.pseg[sg]);
+      else qr = rsrc(qbase_g + a.qseg[sg]);
+    }
+    const int i = l < PL ? l : l - PL;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        l < PL ? pr : qr, (lds_byte*)(smem + stage * STAGE + (l < PL ? 0 : TB * kRowB) + (i * DW + w) * 1024), 16, loff,
+        uint32_t(i) * (l < PL ? pstep : qstep) + uint32_t(kk) * 1024u, 0, 0);
   };
   // the first steps of a tile (past its end: its last step again, into stages nobody reads)
   auto prologue = [&](const Item& it) {
     aim(it);
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) issue(it.k0 + min(s, it.nk - 1), s);
+    for (int s = 0; s < kStages - 1; ++s)
+#pragma unroll
+      for (int l = 0; l < DLOADS; ++l) issue(l, it.k0 + min(s, it.nk - 1), s);
   };
 
   const int frow = lane & 31, fhalf = lane >> 5;
@@ -135,7 +147,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   const int qbase = (TB + wn * (NI * 32) + frow) * kRowB;
   const int slot0 = ((0 + fhalf) ^ swz(frow)) * 16;
   const int slot1 = ((2 + fhalf) ^ swz(frow)) * 16;
-  constexpr int NMF = MI * NI, NRD = MI + NI;
+  constexpr int NMF = MI * NI, NRD = MI + NI;  // MFMAs and fragment reads per 16-wide slice
 
   int g = xcd;
   Item cur, nxt;
@@ -153,48 +165,55 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
-    bf16x8_t pf0[MI], qf0[NI], pf1[MI], qf1[NI];
-    auto read_frags = [&](const uint8_t* sb, int sl, bf16x8_t* pf, bf16x8_t* qf) {
-#pragma unroll
-      for (int i = 0; i < MI; ++i) pf[i] = *reinterpret_cast<const bf16x8_t*>(sb + pbase + i * 32 * kRowB + sl);
-#pragma unroll
-      for (int j = 0; j < NI; ++j) qf[j] = *reinterpret_cast<const bf16x8_t*>(sb + qbase + j * 32 * kRowB + sl);
+    bf16x8_t pf[2][MI], qf[2][NI];  // fragments of the two slices
+    auto read_frag = [&](int r, int stage, int sl) {
+      const uint8_t* sb = smem + stage * STAGE + (sl ? slot1 : slot0);
+      if (r < MI) pf[sl][r] = *reinterpret_cast<const bf16x8_t*>(sb + pbase + r * 32 * kRowB);
+      else qf[sl][r - MI] = *reinterpret_cast<const bf16x8_t*>(sb + qbase + (r - MI) * 32 * kRowB);
     };
-    auto mfma_slice = [&](const bf16x8_t* pf, const bf16x8_t* qf) {
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], pf[i], acc[i][j], 0, 0, 0);
+    auto mfma = [&](int m, int sl) {
+      const int i = m / NI, j = (i & 1) ? NI - 1 - m % NI : m % NI;
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[sl][j], pf[sl][i], acc[i][j], 0, 0, 0);
     };
+    // The order below is the instruction order: left to itself the compiler gathers the loads (which write LDS) between
+    // the LDS reads, and the MFMAs wait behind them. 8192 x 4096 x 128256: 1.19 PFLOP/s so, 1.45 in this order.
     auto main_loop = [&](auto issue_c) {
       constexpr bool ISS = decltype(issue_c)::value;
-      constexpr int L = ISS ? DLOADS : 0;
       const int nk = cur.nk, last = cur.k0 + nk - 1;
       if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 2) * DLOADS);
       __builtin_amdgcn_s_barrier();
-      read_frags(smem, slot0, pf0, qf0);
-      int cs = 0, ns = 1, fs = kStages - 1;
+#pragma unroll
+      for (int r = 0; r < NRD; ++r) read_frag(r, 0, 0);
+      int cs = 0, ns = 1, fs = kStages - 1;  // stages of steps kt, kt + 1, kt + kStages - 1
       for (int kt = 0; kt < nk; ++kt) {
-        read_frags(smem + cs * STAGE, slot1, pf1, qf1);
-        mfma_slice(pf0, qf0);
-        static_assert(NMF >= DLOADS / (NW == 8 ? 1 : 2), "slice schedule");
-#pragma unroll
-        for (int i = 0; i < NMF; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // 1 MFMA
-          if (i < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // 1 LDS read
-        }
-        if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 3) * DLOADS);  // step kt + 1 has landed
+        const int kl = min(cur.k0 + kt + kStages - 1, last);
+        __builtin_amdgcn_sched_barrier(0);
+        // first slice, with the second one's reads and half of the loads
+        static_for<NMF>([&](auto tc) {
+          constexpr int t = decltype(tc)::value;
+          mfma(t, 0);
+          if constexpr (t < NRD) read_frag(t, cs, 1);
+          if constexpr (ISS && t % 2 == 1) issue(t / 2, kl, fs);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        static_assert(DLOADS == NMF, "half of the loads in each half");
+        static_for<NMF / 2>([&](auto tc) {
+          constexpr int t = decltype(tc)::value;
+          mfma(t, 1);
+          if constexpr (ISS) issue(NMF / 2 + t, kl, fs);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 2) * DLOADS);  // step kt + 1 has landed
         __builtin_amdgcn_s_barrier();
-        if constexpr (ISS) issue(min(cur.k0 + kt + kStages - 1, last), fs);
-        read_frags(smem + ns * STAGE, slot0, pf0, qf0);
-        mfma_slice(pf1, qf1);
+        __builtin_amdgcn_sched_barrier(0);
+        // the rest of the second slice, with the next step's first reads
+        static_for<NMF / 2>([&](auto tc) {
+          constexpr int t = decltype(tc)::value, R0 = t * NRD / (NMF / 2), R1 = (t + 1) * NRD / (NMF / 2);
+          mfma(NMF / 2 + t, 1);
 #pragma unroll
-        for (int i = 0; i < NMF; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          if (i < L) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // 1 load
-          if (i < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
+          for (int r = R0; r < R1; ++r) read_frag(r, ns, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        });
         cs = ns;
         ns = (ns + 1 == kStages) ? 0 : ns + 1;
         fs = (fs + 1 == kStages) ? 0 : fs + 1;
@@ -302,6 +321,15 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
 #pragma unroll
           for (int t = 0; t < 4; ++t) acc[q / (NI * 4)][(q >> 2) & 1][4 * (q & 3) + t] += p[t];
         }
+      }
+      if (!a.part) {
+        const float f = out_factor(a.alpha, a.denom);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] *= f;
       }
       if (a.part) {
 #pragma unroll
@@ -593,10 +621,7 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
     loss = (d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
   }
   const float wt = on != 0.0f ? (a.weight ? a.weight[r] : 1.0f) : 0.0f;
-  float gf = a.scale * wt * on * a.inv_t;
-  if (on == 0.0f) gf = 0.0f;
-  else if (a.denom) gf = a.denom[0] != 0.0f ? gf / a.denom[0] : gf * 0.0f;
-  a.row[r] = float4{m, s, gf, 2.0f * a.z_loss * lse};
+  a.row[r] = float4{m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
   if (a.token_loss) a.token_loss[r] = loss;
   if (a.lse) a.lse[r] = on != 0.0f ? lse : 0.0f;
   a.weighted[r] = on != 0.0f ? wt * loss : 0.0f;
@@ -710,6 +735,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
   const int row = bi * TB + (w / G::WN) * (G::MI * 32) + (blk >> 3) * 32 + (ln & 31);
   const int c = bj * TB + (w % G::WN) * 64 + ((blk >> 2) & 1) * 32 + (blk & 3) * 8 + (ln >> 5) * 4;
   if (row >= a.rows || c >= a.cols) return;
+  s *= out_factor(a.alpha, a.denom);
   const int64_t at = int64_t(row) * a.ldo + c;
   if (a.out_bf16) {
     const u32x2 v = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};

@@ -197,7 +197,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     if (a->dw) LOSS_TRY(launch_loss_zero(a->dw, p.v * p.h * es, st), "zero launch");
     return MFSDP_OK;
   }
-  const float inv_t = float(1.0 / l.temperature);
+  const float inv_t = float(1.0 / l.temperature), factor = float(a->scale / l.temperature);
   LossTargets t{};
   t.ids = l.ids;
   t.logits = l.logits;
@@ -300,9 +300,6 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     rw.on = t.on + r0;
     rw.weight = a->token_weight ? a->token_weight + r0 : nullptr;
     rw.zt = z.zt;
-    rw.denom = denom;
-    rw.scale = float(a->scale);
-    rw.inv_t = inv_t;
     rw.z_loss = float(l.z_loss);
     rw.row = reinterpret_cast<float4*>(ws + p.row);
     rw.token_loss = a->token_loss ? a->token_loss + r0 : nullptr;
@@ -341,6 +338,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       m.out = static_cast<uint8_t*>(a->dx) + r0 * p.h * es;
       m.ldo = p.h;
       m.out_bf16 = !p.f32;
+      m.alpha = factor;
+      m.denom = denom;
       if (m.splits > 1) m.part = f32p(p.part);
       LOSS_TRY(launch_loss_gemm(m, kLossOut, p.dx.tile, st), "dx launch");
       if (m.splits > 1) {
@@ -355,6 +354,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
         j.out_bf16 = m.out_bf16;
         j.out = m.out;
         j.ldo = m.ldo;
+        j.alpha = m.alpha;
+        j.denom = m.denom;
         LOSS_TRY(launch_loss_join(j, p.dx.tile, st), "dx join launch");
       }
     }
@@ -365,6 +366,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       m.out = a->dw;
       m.ldo = p.h;
       m.out_bf16 = !p.f32;
+      m.alpha = factor;
+      m.denom = denom;
       if (r0 > 0) m.prev = f32p(p.acc);
       if (r0 + p.chunk < p.n) m.part = f32p(p.acc);
       LOSS_TRY(launch_loss_gemm(m, kLossOut, p.dw.tile, st), "dw launch");

@@ -53,6 +53,8 @@ struct LossGemm {
   int32_t out_bf16;
   float* part;
   const float* prev;
+  float alpha;                                     // result = alpha / denom[0] (denom null: 1) P Q^T (part: P Q^T)
+  const float* denom;
 };
 
 // Panel-blocked bf16 copies of a row-major R x C matrix: as it is (dst, ldn columns) and transposed (dst_t, ldt columns),
@@ -82,21 +84,22 @@ struct LossTargets {
   float *q, *ent, *on;
 };
 
-// Per row of a chunk: the row's softmax (largest logit M, sum s of the others' exp relative to it), its loss and the
-// factor of its gradient.
+// Per row of a chunk: the row's softmax (largest logit M, sum s of the others' exp relative to it), its loss and its weight
+// in the gradient.
 struct LossRows {
   const float *gm, *gs;
   int64_t ldr;
   int32_t groups, rows, rows_pad, k;
   const int32_t* id;
-  const float *q, *ent, *on, *weight, *zt, *denom;  // denom: one float, or null
-  float scale, inv_t, z_loss;
-  float4* row;                 // {M, s, g / T, 2 z_loss lse}
+  const float *q, *ent, *on, *weight, *zt;
+  float z_loss;
+  float4* row;                 // {M, s, weight, 2 z_loss lse}
   float *token_loss, *lse;     // optional
   float* weighted;             // weight x loss
 };
 
-// dz of a chunk: codes -> bf16 in place and transposed, or fp32 logits -> three bf16 parts and their transposes.
+// dz of a chunk, without the factor scale / (T D) common to all tokens (which the products apply: rounded with it, the
+// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place and transposed, or fp32 logits -> three bf16 parts and their transposes.
 struct LossGrad {
   uint16_t* codes;
   const float* logits;
@@ -116,6 +119,8 @@ struct LossJoin {
   int32_t splits, tiles, tm, tn, rows, cols, out_bf16;
   void* out;
   int64_t ldo;
+  float alpha;
+  const float* denom;
 };
 
 enum { kLossLogits = 0, kLossOut = 1 };
