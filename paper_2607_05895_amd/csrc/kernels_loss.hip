@@ -67,8 +67,13 @@ __device__ __forceinline__ float out_factor(float alpha, const float* denom) {
   return d != 0.0f ? alpha / d : 0.0f;
 }
 
+// two logits' 16-bit codes from their distances in [0, 1]
+__device__ __forceinline__ uint32_t code2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(a, b));
+}
+
 struct Item {
-  int bi, bj, k0, nk;
+  int p, bi, bj, k0, nk;  // problem, tile, K steps
 };
 
 // C = P Q^T on a persistent grid. The main loop is the one of the Newton-Schulz products: a five-stage LDS ring filled by
@@ -77,7 +82,7 @@ struct Item {
 // issued before this tile's epilogue. Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
 // column); the order is arithmetic, so a launch needs no schedule in memory.
 template <int NW, int TB, int NSEG, int KIND>
-__global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm a) {
+__global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm2 b) {
   using G = Grid<NW, TB>;
   constexpr int MI = G::MI, NI = G::NI, STAGE = G::STAGE, DW = G::DW, PL = G::PL, DLOADS = G::DLOADS;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * STAGE];
@@ -85,14 +90,18 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / G::WN, wn = w % G::WN;
   const int xcd = blockIdx.x % kGemmXcds, slot = blockIdx.x / kGemmXcds;
-  const int tiles = a.tm * a.tn, total = tiles * a.splits;
+  const int first = b.g[0].tm * b.g[0].tn * b.g[0].splits;
+  const int total = first + (KIND == kLossOut && b.count > 1 ? b.g[1].tm * b.g[1].tn * b.g[1].splits : 0);
   const int per = min(G::SLOTS, (total + kGemmXcds - 1) / kGemmXcds);  // tiles of one group
   if (slot >= per) return;
-  const int steps = NSEG * a.nk;
 
   auto item_at = [&](int g, Item& it) -> bool {
-    const int i = g * per + slot;
+    int i = g * per + slot;
     if (i >= total) return false;
+    it.p = KIND == kLossOut && i >= first ? 1 : 0;
+    const LossGemm& a = b.g[it.p];
+    if (it.p) i -= first;
+    const int tiles = a.tm * a.tn, steps = NSEG * a.nk;
     const int s = i / tiles, j = i - s * tiles;
     const int band = j / (G::BAND * a.tn), r0 = band * G::BAND, hb = min(G::BAND, a.tm - r0);
     const int jj = j - r0 * a.tn;
@@ -107,11 +116,16 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   // load i of P (of Q) of issuing wave w moves the 1 KiB block of 16-row panel i DW + w: lane l its row l / 4, 16-byte chunk
   // (l % 4) ^ swz(row), so that the fragment reads are conflict-free. One lane offset for all; the rest is scalar.
   const uint32_t loff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
-  const uint32_t pstep = DW * kBlkRows * 2 * uint32_t(a.ldp), qstep = DW * kBlkRows * 2 * uint32_t(a.ldq);
+  uint32_t pstep = 0, qstep = 0;
+  int lp = 0;  // its problem
   const uint16_t *pbase_g = nullptr, *qbase_g = nullptr;  // the wave's first panels of the tile being loaded
   __amdgpu_buffer_rsrc_t pr, qr;
   auto rsrc = [](const uint16_t* p) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00020000); };
   auto aim = [&](const Item& it) {
+    const LossGemm& a = b.g[it.p];
+    lp = it.p;
+    pstep = DW * kBlkRows * 2 * uint32_t(a.ldp);
+    qstep = DW * kBlkRows * 2 * uint32_t(a.ldq);
     pbase_g = a.P + (int64_t(it.bi) * TB + w * kBlkRows) * a.ldp;
     qbase_g = a.Q + (int64_t(it.bj) * TB + w * kBlkRows) * a.ldq;
     if constexpr (NSEG == 1) {
@@ -123,6 +137,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   auto issue = [&](int l, int k, int stage) {
     int kk = k;
     if constexpr (NSEG > 1) {
+      const LossGemm& a = b.g[lp];
       const int sg = k / a.nk;
       kk = k - sg * a.nk;
       if (l < PL) pr = rsrc(pbase_g + a.pseg[sg]);
@@ -234,6 +249,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     int ln = lane;
     asm volatile("" : "+v"(ln));  // lane-dependent offsets are formed here, not kept through the main loop
     const int er = ln & 31, eh = ln >> 5;
+    const LossGemm& a = b.g[cur.p];
     if constexpr (KIND == kLossLogits) {
       const int c0 = cur.bj * TB + wn * 64;       // the wave's first column
       const int left = a.cols - c0;               // real columns from there
@@ -243,61 +259,81 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
                ((c & 7) << 1);
       };
       const int wr_base = slab_off(wm * 32 + er, wn * 64 + eh * 4);
+      const int row0 = cur.bi * TB + wm * (MI * 32) + er;
+      // the rows' first targets, all asked for before any is needed
+      int id0[MI];
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) id0[mi] = *(gptr<const int32_t>)(a.ids + int64_t(row0 + mi * 32) * a.k);
+      const float L = kLog2e * a.inv_t;
+      if (left < 64) {  // columns past the vocabulary
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if ((e >> 4) * 32 + ((e & 15) >> 2) * 8 + eh * 4 + (e & 3) >= left) {
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) acc[mi][e >> 4][e & 15] = -__builtin_inff();
+          }
+      }
       static_for<MI>([&](auto mi_c) {
         constexpr int mi = decltype(mi_c)::value;
-        const int row = cur.bi * TB + wm * (MI * 32) + mi * 32 + er;
-        float u[32];
-        float m = -__builtin_inff();
+        const int row = row0 + mi * 32;
+        float u[32];  // logits before the temperature
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          u[e] = acc[mi][e >> 4][e & 15] * a.inv_t;
-          if (left < 64 && (e >> 4) * 32 + ((e & 15) >> 2) * 8 + eh * 4 + (e & 3) >= left) u[e] = -__builtin_inff();
-          m = fmaxf(m, u[e]);
-        }
+        for (int e = 0; e < 32; ++e) u[e] = acc[mi][e >> 4][e & 15];
+        float m = u[0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) m = fmaxf(m, u[e]);
         m = fmaxf(m, __shfl_xor(m, 32));
-        // sum of the others' exp: the largest term itself is 1, and what is far below it must not vanish in that 1
-        float s = 0.0f, ones = 0.0f;
+        // Sum of the others' exp: the largest term itself is 1, and what is far below it must not vanish in that 1. A
+        // term's fraction is the term, but 0 for a 1; how many ones there are (equal logits) is what the two sums differ by.
+        float s = 0.0f, all = 0.0f;
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-          const bool top = u[e] == m;
-          const float x = __builtin_amdgcn_exp2f((u[e] - m) * kLog2e);
-          s += top ? 0.0f : x;
-          ones += top ? 1.0f : 0.0f;
+          const float x = __builtin_amdgcn_exp2f((u[e] - m) * L);
+          s += __builtin_amdgcn_fractf(x);
+          all += x;
         }
+        float ones = __builtin_rintf(all - s);
         s += __shfl_xor(s, 32);
         ones += __shfl_xor(ones, 32);
         if (left > 0 && eh == 0) {
           const int64_t at = int64_t(c0 >> 6) * a.ldr + row;
-          a.gm[at] = m;
+          a.gm[at] = m * a.inv_t;
           a.gs[at] = s + (ones - 1.0f);
         }
-        for (int j = 0; j < a.k; ++j) {
-          const int id = a.ids[int64_t(row) * a.k + j] - c0;
-          if (id >= 0 && id < 64 && ((id >> 2) & 1) == eh) {
-            const int e = (id >> 5) * 16 + ((id >> 3) & 3) * 4 + (id & 3);
+        auto target = [&](int id, int j) {
+          const int x = (id - c0) ^ (eh << 2);  // in this lane's columns: bits 0, 1, 3, 4, 5
+          if ((x & ~0x3b) == 0) {
+            const int e = (x >> 5) * 16 + ((x >> 3) & 3) * 4 + (x & 3);
             float z = 0.0f;
 #pragma unroll
             for (int f = 0; f < 32; ++f) z = e == f ? u[f] : z;
-            a.zt[int64_t(row) * a.k + j] = z;
+            a.zt[int64_t(row) * a.k + j] = z * a.inv_t;
           }
+        };
+        target(id0[mi], 0);
+        for (int j = 1; j < a.k; j += 4) {
+          int id[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) id[i] = j + i < a.k ? a.ids[int64_t(row) * a.k + j + i] : -1;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) target(id[i], j + i);
         }
         if (a.logits) {
           float* dst = a.logits + int64_t(row) * a.ldc + c0;
 #pragma unroll
           for (int p = 0; p < 8; ++p)
             *(gptr<f32x4_t>)(dst + (p >> 2) * 32 + (p & 3) * 8 + eh * 4) =
-                f32x4_t{u[4 * p], u[4 * p + 1], u[4 * p + 2], u[4 * p + 3]};
+                f32x4_t{u[4 * p] * a.inv_t, u[4 * p + 1] * a.inv_t, u[4 * p + 2] * a.inv_t, u[4 * p + 3] * a.inv_t};
         }
         if (a.codes) {
+          // round(65535 x) for x in [0, 1], clamped: x = 1 is kLossOctaves factors of two below the largest
+          const float C = -L * (1.0f / kLossOctaves);
 #pragma unroll
-          for (int p = 0; p < 8; ++p) {
-            uint32_t q[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-              q[t] = uint32_t(__builtin_rintf(fminf((m - u[4 * p + t]) * (kLossCodeStep * kLog2e), 65535.0f)));
+          for (int p = 0; p < 8; ++p)
             *(lptr<u32x2>)(slab + wr_base + (p >> 2) * 1024 + ((((p & 3) ^ wsw) - wsw) << 4)) =
-                u32x2{q[0] | q[1] << 16, q[2] | q[3] << 16};
-          }
+                u32x2{code2((u[4 * p] - m) * C, (u[4 * p + 1] - m) * C), code2((u[4 * p + 2] - m) * C, (u[4 * p + 3] - m) * C)};
+        }
+        if (a.codes) {
           LOSS_WAIT_LGKM0();
           __builtin_amdgcn_s_barrier();
           const int rin = ln >> 2, ch = ln & 3;
@@ -427,14 +463,102 @@ __device__ __forceinline__ u32x4 split8(float (&x)[8]) {
   return o;
 }
 
-// One 32 x 256 tile per workgroup of 256: four 8-column chunks per thread (row it * 8 + t / 32, chunk t % 32).
-__global__ __launch_bounds__(256) void loss_pack_kernel(const LossPack2 b) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
+// Label entry `at` (token times k plus slot): its id; its teacher logit; whether it makes its token count.
+__device__ __forceinline__ int64_t label_id(const LossLabels& l, int64_t at) {
+  return l.id64 ? ((const int64_t*)l.ids)[at] : int64_t(((const int32_t*)l.ids)[at]);
+}
+__device__ __forceinline__ float label_logit(const LossLabels& l, int64_t at) {
+  return l.logits_bf16 ? __uint_as_float(uint32_t(((const uint16_t*)l.logits)[at]) << 16) : ((const float*)l.logits)[at];
+}
+__device__ __forceinline__ bool slot_counts(const LossLabels& l, int64_t at) {
+  const int64_t id = label_id(l, at);
+  return l.logits ? id >= 0 && !(label_logit(l, at) == -__builtin_inff()) : id != l.ignore;
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// The labels of token r (< n_pad) in one form: one wave, lanes over the slots.
+__device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
+  const int ln = threadIdx.x & 63;
+  const LossLabels& l = a.l;
+  constexpr int PER = kLossMaxTop / 64;
+  float lg[PER], m = -__builtin_inff();
+  int id[PER];
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * 64 + ln;
+    id[i] = -1;
+    lg[i] = -__builtin_inff();
+    if (r < l.n && j < l.k) {
+      const int64_t at = r * l.k + j;
+      const int64_t v = label_id(l, at);
+      const bool none = l.logits ? v < 0 : v == l.ignore;
+      if (!none) {
+        bad |= v < 0 || v >= l.v;
+        id[i] = v >= 0 && v < l.v ? int(v) : -1;
+        lg[i] = !l.logits ? 0.0f : label_logit(l, at) * l.inv_t;
+        m = fmaxf(m, lg[i]);
+        if (!(lg[i] == lg[i])) bad = true;  // a NaN teacher logit
+      }
+    }
+  }
+  m = wave_max(m);
+  bad = __any(bad);
+  // (a row whose slots are all empty, or all of logit -inf, teaches nothing)
+  const bool on = m > -__builtin_inff();
+  float e[PER], s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    e[i] = on && lg[i] > -__builtin_inff() ? expf(lg[i] - m) : 0.0f;
+    s += e[i];
+  }
+  s = wave_sum(s);
+  float ent = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * 64 + ln;
+    const float q = on ? e[i] / s : 0.0f;
+    if (q > 0.0f) ent += q * ((lg[i] - m) - logf(s));
+    if (j < l.k) {
+      a.id[r * l.k + j] = on ? id[i] : -1;
+      a.q[r * l.k + j] = q;
+    }
+  }
+  ent = wave_sum(ent);
+  if (ln == 0) {
+    a.ent[r] = ent;
+    a.on[r] = bad ? __builtin_nanf("") : on ? 1.0f : 0.0f;
+  }
+}
+
+// One 32 x 256 tile of a packed operand: four 8-column chunks per thread (row it * 8 + t / 32, chunk t % 32).
+__device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, uint8_t* smem, int* counts) {
   lds_byte* tile = (lds_byte*)smem;
-  const LossPack& d = b.d[b.count > 1 && int(blockIdx.x) >= b.d[1].blocks_begin ? 1 : 0];
   const int64_t i = int(blockIdx.x) - d.blocks_begin;
   const int64_t tc = d.cols / 256, r0 = i / tc * 32, c0 = i % tc * 256;
   const int t = threadIdx.x, ch = t & 31;
+  uint32_t skip = 0;  // rows of the tile whose token does not count
+  if (d.label_row >= 0) {
+    if (t < 32) counts[t] = 0;
+    __syncthreads();
+    for (int e = t; e < 32 * a.l.k; e += 256) {
+      const int r = e / a.l.k;
+      if (r0 + r < d.R && slot_counts(a.l, (d.label_row + r0 + r) * a.l.k + (e - r * a.l.k))) counts[r] = 1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) skip |= counts[it * 8 + (t >> 5)] ? 0u : 1u << it;
+  }
   const int64_t c = c0 + ch * 8;
   float x[4][8];
 #pragma unroll
@@ -442,7 +566,7 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(const LossPack2 b) {
     const int64_t r = r0 + it * 8 + (t >> 5);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[it][e] = 0.0f;
-    if (r < d.R && c < d.C && !(d.row_on && d.row_on[r] == 0.0f)) {
+    if (r < d.R && c < d.C && !(skip >> it & 1)) {
       const int64_t at = r * d.C + c;
       if (d.bf16) {
         const uint16_t* p = (const uint16_t*)d.src + at;
@@ -497,92 +621,30 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(const LossPack2 b) {
   }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
-
-// One wave per token, lanes over its slots.
-__global__ __launch_bounds__(256) void loss_targets_kernel(const LossTargets a) {
-  const int ln = threadIdx.x & 63;
-  const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (r >= a.n_pad) return;
-  constexpr int PER = kLossMaxTop / 64;
-  float lg[PER], m = -__builtin_inff();
-  int id[PER];
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int j = i * 64 + ln;
-    id[i] = -1;
-    lg[i] = -__builtin_inff();
-    if (r < a.n && j < a.k) {
-      const int64_t at = r * a.k + j;
-      const int64_t v = a.id64 ? ((const int64_t*)a.ids)[at] : int64_t(((const int32_t*)a.ids)[at]);
-      const bool none = a.logits ? v < 0 : v == a.ignore;
-      if (!none) {
-        bad |= v < 0 || v >= a.v;
-        id[i] = v >= 0 && v < a.v ? int(v) : -1;
-        lg[i] = !a.logits ? 0.0f
-                : (a.logits_bf16 ? __uint_as_float(uint32_t(((const uint16_t*)a.logits)[at]) << 16)
-                                 : ((const float*)a.logits)[at]) * a.inv_t;
-        m = fmaxf(m, lg[i]);
-        if (!(lg[i] == lg[i])) bad = true;  // a NaN teacher logit
-      }
-    }
+__global__ __launch_bounds__(256) void loss_prep_kernel(const LossPrep a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
+  __shared__ int counts[32];
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.counter) *a.counter = 0;
+  if (int(blockIdx.x) < a.label_blocks) {
+    const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (r < a.n_pad) prep_labels(a, r);
+    return;
   }
-  m = wave_max(m);
-  bad = __any(bad);
-  // (a row whose slots are all empty, or all of logit -inf, teaches nothing)
-  const bool on = m > -__builtin_inff();
-  float e[PER], s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    e[i] = on && lg[i] > -__builtin_inff() ? expf(lg[i] - m) : 0.0f;
-    s += e[i];
-  }
-  s = wave_sum(s);
-  float ent = 0.0f;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int j = i * 64 + ln;
-    const float q = on ? e[i] / s : 0.0f;
-    if (q > 0.0f) ent += q * ((lg[i] - m) - logf(s));
-    if (j < a.k) {
-      a.id[r * a.k + j] = on ? id[i] : -1;
-      a.q[r * a.k + j] = q;
-    }
-  }
-  ent = wave_sum(ent);
-  if (ln == 0) {
-    a.ent[r] = ent;
-    a.on[r] = bad ? __builtin_nanf("") : on ? 1.0f : 0.0f;
-  }
+  prep_pack(a, a.d[a.packs > 1 && int(blockIdx.x) >= a.d[1].blocks_begin ? 1 : 0], smem, counts);
 }
 
-// One workgroup of 1024: a sum in a fixed order (64-bit, so that it does not depend on how many there are).
-__global__ __launch_bounds__(1024) void loss_sum_kernel(const float* a, const float* b, int64_t n, float scale,
-                                                        const float* denom, float* out) {
-  __shared__ double part[16];
+// Sum over a workgroup, in 64 bits and a fixed order, of n values (times b where a value is not 0); for every thread.
+template <int T>
+__device__ __forceinline__ double block_sum(const float* a, const float* b, int64_t n, double* part) {
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) s += b && a[i] != 0.0f ? double(a[i]) * b[i] : double(a[i]);
+  for (int64_t i = threadIdx.x; i < n; i += T) s += b && a[i] != 0.0f ? double(a[i]) * b[i] : double(a[i]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0;
-    for (int i = 0; i < 16; ++i) s += part[i];
-    s *= scale;
-    if (denom) s = denom[0] != 0.0f ? s / denom[0] : (s == s ? 0.0 : s);
-    out[0] = float(s);
-  }
+  s = 0.0;
+  for (int i = 0; i < T / 64; ++i) s += part[i];
+  return s;
 }
 
 // (m, s) of two sets joined: m the largest, s the sum of exp(. - m) over all others.
@@ -593,38 +655,77 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
   m = hi;
 }
 
-// 32 rows per workgroup of 1024: thread t goes through groups t / 32, + 32, ... of row t % 32.
+// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB, four at a time.
+template <int RPB>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
-  __shared__ float sm[32][33], ss[32][33];
-  const int rl = threadIdx.x & 31, gl = threadIdx.x >> 5;
-  const int64_t r = int64_t(blockIdx.x) * 32 + rl;
-  float m = -__builtin_inff(), s = 0.0f;
-  for (int g = gl; g < a.groups; g += 32) join_softmax(m, s, a.gm[g * a.ldr + r], a.gs[g * a.ldr + r]);
-  sm[gl][rl] = m;
-  ss[gl][rl] = s;
-  __syncthreads();
-  if (gl != 0) return;
-  for (int i = 1; i < 32; ++i) join_softmax(m, s, sm[i][rl], ss[i][rl]);
-  if (r >= a.rows) {
-    a.row[r] = float4{0.0f, 0.0f, 0.0f, 0.0f};
-    return;
-  }
-  const float on = a.on[r];
-  const float ls = log1pf(s), lse = m + ls;
-  float loss = 0.0f;
-  if (on != 0.0f) {
-    float d = a.ent[r];
-    for (int j = 0; j < a.k; ++j) {
-      const float q = a.q[r * a.k + j];
-      if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (m - a.zt[r * a.k + j]);
+  constexpr int GS = 1024 / RPB;
+  __shared__ float sm[GS][RPB + 1], ss[GS][RPB + 1];
+  __shared__ double part[16];
+  __shared__ int last;
+  const int blocks = a.rows_pad / RPB;
+  if (int(blockIdx.x) == blocks) {  // (the extra workgroup)
+    const double d = block_sum<1024>(a.all_on, a.all_weight, a.n, part);
+    if (threadIdx.x == 0) a.denom[0] = float(d);
+  } else {
+    const int rl = threadIdx.x % RPB, gl = threadIdx.x / RPB;
+    const int64_t r = int64_t(blockIdx.x) * RPB + rl;
+    const float none = -__builtin_inff();
+    float m = none, s = 0.0f;
+    for (int g = gl; g < a.groups; g += 4 * GS) {
+      float gm[4], gs[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = g + i * GS < a.groups;
+        gm[i] = in ? a.gm[(g + i * GS) * a.ldr + r] : none;
+        gs[i] = in ? a.gs[(g + i * GS) * a.ldr + r] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) join_softmax(m, s, gm[i], gs[i]);
     }
-    loss = (d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
+    sm[gl][rl] = m;
+    ss[gl][rl] = s;
+#pragma unroll
+    for (int o = GS / 2; o > 0; o >>= 1) {
+      __syncthreads();
+      if (gl < o) {
+        join_softmax(m, s, sm[gl + o][rl], ss[gl + o][rl]);
+        sm[gl][rl] = m;
+        ss[gl][rl] = s;
+      }
+    }
+    if (gl == 0) {
+      if (r >= a.rows) {
+        a.row[r] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+      } else {
+        const float on = a.on[r];
+        const float ls = log1pf(s), lse = m + ls;
+        float loss = 0.0f;
+        if (on != 0.0f) {
+          float d = a.ent[r];
+          for (int j = 0; j < a.k; ++j) {
+            const float q = a.q[r * a.k + j];
+            if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (m - a.zt[r * a.k + j]);
+          }
+          loss = (d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
+        }
+        const float wt = on != 0.0f ? (a.weight ? a.weight[r] : 1.0f) : 0.0f;
+        a.row[r] = float4{m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
+        if (a.token_loss) a.token_loss[r] = loss;
+        if (a.lse) a.lse[r] = on != 0.0f ? lse : 0.0f;
+        a.weighted[r] = on != 0.0f ? wt * loss : 0.0f;
+      }
+    }
   }
-  const float wt = on != 0.0f ? (a.weight ? a.weight[r] : 1.0f) : 0.0f;
-  a.row[r] = float4{m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
-  if (a.token_loss) a.token_loss[r] = loss;
-  if (a.lse) a.lse[r] = on != 0.0f ? lse : 0.0f;
-  a.weighted[r] = on != 0.0f ? wt * loss : 0.0f;
+  if (!a.loss) return;
+  // the workgroup that ends last, of every chunk's launches, sees all the others' results
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(a.counter, 1) + 1 == a.last;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  const double t = block_sum<1024>(a.all_weighted, nullptr, a.n, part) * a.scale;
+  if (threadIdx.x == 0) a.loss[0] = float(!a.denom_in ? t : a.denom_in[0] != 0.0f ? t / a.denom_in[0] : t == t ? 0.0 : t);
 }
 
 // One 32 x 256 tile of dz per workgroup of 256: from the logits to LDS, the targets' elements there from their fp32 logits,
@@ -658,12 +759,12 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
       for (int e = 0; e < 8; ++e) fix[r * 256 + cl + e] = x[e];
     } else {
       const u32x4 v = *(gptr<const u32x4>)(a.codes + blk_index(row, c, a.ldc));
-      const float m = c < a.v ? a.gm[(c >> 6) * a.ldr + row] : 0.0f;
+      const float m = c < a.v ? a.gm[(c >> a.group_shift) * a.ldr + row] : 0.0f;
       const float base = (m - rw.x) * kLog2e;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t q = v[e >> 1] >> (16 * (e & 1)) & 0xffff;
-        const float p = q == 65535u ? 0.0f : __builtin_amdgcn_exp2f(base - float(q) * (1.0f / kLossCodeStep));
+        const float p = q == 65535u ? 0.0f : __builtin_amdgcn_exp2f(base - float(q) * (kLossOctaves / 65535.0f));
         x[e] = rw.z != 0.0f && c + e < a.v ? p * f : 0.0f;
       }
       *(lptr<u32x4>)(tile + tile_off(r, cl)) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
@@ -721,6 +822,30 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   }
 }
 
+// Elements at .. + 3 (the first `left` of them) of a row-major bf16 or fp32 tensor.
+__device__ __forceinline__ void store4(void* out, int bf16, int64_t at, f32x4_t s, int left) {
+  if (bf16) {
+    const u32x2 v = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+    uint16_t* o = (uint16_t*)out + at;
+    if (left >= 4) {
+      *(gptr<u32x2_a2>)o = v;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (t < left) o[t] = uint16_t(v[t >> 1] >> (16 * (t & 1)));
+    }
+  } else {
+    float* o = (float*)out + at;
+    if (left >= 4) {
+      *(gptr<f32x4_a4>)o = s;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (t < left) o[t] = s[t];
+    }
+  }
+}
+
 // The K ranges' partial tiles added in order; four elements per thread.
 template <int NW, int TB>
 __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
@@ -736,27 +861,190 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
   const int c = bj * TB + (w % G::WN) * 64 + ((blk >> 2) & 1) * 32 + (blk & 3) * 8 + (ln >> 5) * 4;
   if (row >= a.rows || c >= a.cols) return;
   s *= out_factor(a.alpha, a.denom);
-  const int64_t at = int64_t(row) * a.ldo + c;
-  if (a.out_bf16) {
-    const u32x2 v = {pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
-    uint16_t* o = (uint16_t*)a.out + at;
-    if (c + 4 <= a.cols) {
-      *(gptr<u32x2_a2>)o = v;
-    } else {
+  store4(a.out, a.out_bf16, int64_t(row) * a.ldo + c, s, a.cols - c);
+}
+
+// Products for at most 32 MI tokens with w as it lies (LossStream). Eight waves, each all rows by 32 of the tile's 256
+// columns; K in steps of 64 through a ring of NST stages filled NST - 1 steps ahead by direct loads. Bound by HBM: w is read
+// once, 32 KiB per step, with up to (NST - 1) steps of it in flight per CU.
+// logits: a stage holds 256 rows of w by 64 of h (128-byte rows of eight 16-byte chunks, chunk c of row r in slot c ^ (r / 2) % 8).
+// dx: 64 rows of w by 256 of h (512-byte rows, chunk c in slot c ^ 2 (r % 4)), its fragments read transposed.
+// Past a row's end lie the next row's values, past w's end its last ones: they meet zeros of x or dz, or belong to columns
+// that are not stored.
+template <int MI, int KIND>
+__global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a) {
+  constexpr int PB = MI * 32 * 128, QB = 256 * 128, STAGE = PB + QB;
+  constexpr int NST = MI <= 2 ? 4 : 3;
+  constexpr int PL = MI < 2 ? 1 : MI / 2, LOADS = PL + 4;  // per wave and step (MI = 1: two waves load the same)
+  static_assert(NST * STAGE <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[NST * STAGE];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int total = a.tiles * a.splits;
+  const int64_t wrow = a.h * 2;  // bytes
+  const uint32_t ploff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
+  const uint32_t qloff = KIND == kLossLogits
+                             ? uint32_t((lane >> 3) * wrow) + ((lane & 7) ^ (((w & 1) * 4 + (lane >> 4)) & 7)) * 16
+                             : uint32_t((lane >> 5) * wrow) + ((lane & 31) ^ (((w & 1) * 2 + (lane >> 5)) << 1)) * 16;
+  // w from row r0 on; its loads are held to its last 16 bytes (whole chunks are in or out: h is a multiple of 8)
+  uint32_t qmost = 0;
+  auto rows_from = [&](int64_t r0) {
+    const int64_t bytes = (a.v - r0) * wrow, some = bytes < 0x7ffffff0 ? bytes : 0x7ffffff0;
+    qmost = uint32_t(some) - 16;
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.w + r0 * wrow), 0, uint32_t(some), 0x00020000);
+  };
+  auto issue = [&](int tile, int k, int stage) {
+    lds_byte* sb = (lds_byte*)(smem + stage * STAGE);
+    const __amdgpu_buffer_rsrc_t pr = __builtin_amdgcn_make_buffer_rsrc((void*)a.P, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (c + t < a.cols) o[t] = uint16_t(v[t >> 1] >> (16 * (t & 1)));
+    for (int i = 0; i < PL; ++i) {
+      const int b = (i * 8 + w) % (MI * 4), kb = b / (MI * 2), panel = b % (MI * 2);  // K half, 16-row panel
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, sb + kb * (PB / 2) + panel * 1024, 16, ploff,
+                                               uint32_t(panel) * uint32_t(a.ldp * 32) + uint32_t(k * 2 + kb) * 1024u, 0, 0);
     }
-  } else {
-    float* o = (float*)a.out + at;
-    if (c + 4 <= a.cols) {
-      *(gptr<f32x4_a4>)o = s;
-    } else {
+    const __amdgpu_buffer_rsrc_t qr = rows_from(KIND == kLossLogits ? int64_t(tile) * 256 : int64_t(k) * 64);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (c + t < a.cols) o[t] = s[t];
+    for (int i = 0; i < 4; ++i) {  // logits: rows 8 (8 i + w) .. + 7; dx: rows 2 (8 i + w), + 1
+      const uint32_t at = KIND == kLossLogits ? uint32_t((i * 8 + w) * 8 * wrow) + uint32_t(k) * 128u
+                                              : uint32_t((i * 8 + w) * 2 * wrow) + uint32_t(tile) * 512u;
+      const uint32_t off = qloff + at;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, sb + PB + (i * 8 + w) * 1024, 16, off < qmost ? off : qmost, 0, 0, 0);
     }
+  };
+  const int fr = lane & 31, fh = lane >> 5;
+  int item = blockIdx.x;
+  if (item >= total) return;
+  auto range = [&](int it, int& k0, int& nk) {
+    const int s = it / a.tiles;
+    k0 = s * a.kper;
+    nk = min(a.kper, a.nk - k0);
+    return it - s * a.tiles;
+  };
+  int k0, nk, tile = range(item, k0, nk);
+#pragma unroll
+  for (int s = 0; s < NST - 1; ++s) issue(tile, k0 + min(s, nk - 1), s);
+  while (true) {
+    f32x16_t acc[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][v] = 0.0f;
+    int cs = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+      LOSS_WAIT_VMCNT((NST - 2) * LOADS);  // this wave's loads of step kt
+      __builtin_amdgcn_s_barrier();        // everybody's; and step kt - 1 is read
+      issue(tile, k0 + min(kt + NST - 1, nk - 1), cs == 0 ? NST - 1 : cs - 1);
+      const uint8_t* sb = smem + cs * STAGE;
+#pragma unroll
+      for (int sl = 0; sl < 4; ++sl) {  // 16 of K
+        bf16x8_t qf;
+        if constexpr (KIND == kLossLogits) {
+          const int row = w * 32 + fr, c = sl * 2 + fh;
+          qf = *reinterpret_cast<const bf16x8_t*>(sb + PB + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
+        } else {
+          const int grp = lane >> 4, i = lane & 15, row = sl * 16 + (grp >> 1) * 8 + (i >> 2);
+          const int sl16 = w * 4 + (grp & 1) * 2 + ((i & 3) >> 1);
+          lds_byte* q = (lds_byte*)(smem + cs * STAGE + PB) + row * 512 + ((sl16 ^ ((row & 3) << 1)) << 4) + (i & 1) * 8;
+          const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)q);
+          const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)(q + 4 * 512));
+          qf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(sb + (sl >> 1) * (PB / 2) + (i * 32 + fr) * kRowB +
+                                                                 ((((sl & 1) * 2 + fh) ^ swz(fr)) << 4));
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, pf, acc[i], 0, 0, 0);
+        }
+      }
+      cs = cs + 1 == NST ? 0 : cs + 1;
+    }
+    LOSS_WAIT_VMCNT(0);
+    __builtin_amdgcn_s_barrier();
+    const int done = tile, split = item / a.tiles;
+    item += gridDim.x;
+    const bool more = item < total;
+    if (more) {
+      tile = range(item, k0, nk);
+#pragma unroll
+      for (int s = 0; s < NST - 1; ++s) issue(tile, k0 + min(s, nk - 1), s);
+    }
+    // acc[i][4 g + t]: row 32 i + lane % 32, column 8 g + 4 (lane / 32) + t of the wave's 32
+    if constexpr (KIND == kLossLogits) {
+      const int c0 = done * 256 + w * 32, left = int(a.v) - c0;
+      const float L = kLog2e * a.inv_t;
+      if (left > 0) {
+        static_for<MI>([&](auto mi_c) {
+          constexpr int mi = decltype(mi_c)::value;
+          const int row = mi * 32 + fr;
+          float u[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            u[e] = acc[mi][e];
+            if (left < 32 && (e >> 2) * 8 + fh * 4 + (e & 3) >= left) u[e] = -__builtin_inff();
+          }
+          float m = u[0];
+#pragma unroll
+          for (int e = 1; e < 16; ++e) m = fmaxf(m, u[e]);
+          m = fmaxf(m, __shfl_xor(m, 32));
+          float s = 0.0f, all = 0.0f;  // as in loss_gemm_kernel
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = __builtin_amdgcn_exp2f((u[e] - m) * L);
+            s += __builtin_amdgcn_fractf(x);
+            all += x;
+          }
+          float ones = __builtin_rintf(all - s);
+          s += __shfl_xor(s, 32);
+          ones += __shfl_xor(ones, 32);
+          if (fh == 0) {
+            const int64_t at = int64_t(c0 >> 5) * a.ldr + row;
+            a.gm[at] = m * a.inv_t;
+            a.gs[at] = s + (ones - 1.0f);
+          }
+          for (int j = 0; j < a.k; ++j) {
+            const int x = (a.ids[row * a.k + j] - c0) ^ (fh << 2);
+            if ((x & ~0x1b) == 0) {
+              const int e = ((x >> 3) & 3) * 4 + (x & 3);
+              float z = 0.0f;
+#pragma unroll
+              for (int f = 0; f < 16; ++f) z = e == f ? u[f] : z;
+              a.zt[row * a.k + j] = z * a.inv_t;
+            }
+          }
+          if (a.codes) {
+            const float C = -L * (1.0f / kLossOctaves);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              *(gptr<u32x2>)(a.codes + blk_index(row, c0 + g * 8 + fh * 4, a.ldc)) =
+                  u32x2{code2((u[4 * g] - m) * C, (u[4 * g + 1] - m) * C), code2((u[4 * g + 2] - m) * C, (u[4 * g + 3] - m) * C)};
+          }
+        });
+      }
+    } else {
+      float* part = a.part + int64_t(split) * (MI * 32) * a.ldo + done * 256 + w * 32;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(gptr<f32x4_t>)(part + (i * 32 + fr) * a.ldo + g * 8 + fh * 4) =
+              f32x4_t{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+    }
+    if (!more) break;
   }
+  LOSS_WAIT_VMCNT(0);
+}
+
+// The K ranges' row-major results added in order: four columns per thread.
+__global__ __launch_bounds__(256) void loss_join_rows_kernel(const LossJoin a) {
+  const int per = (a.cols + 3) / 4;
+  const int64_t q = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t row = q / per;
+  const int c = int(q - row * per) * 4;
+  if (row >= a.rows) return;
+  const float* p = a.part + row * a.ldp + c;
+  f32x4_t s = *(gptr<const f32x4_t>)p;
+  for (int i = 1; i < a.splits; ++i) s += *(gptr<const f32x4_t>)(p + i * a.stride);
+  s *= out_factor(a.alpha, a.denom);
+  store4(a.out, a.out_bf16, row * a.ldo + c, s, a.cols - c);
 }
 
 __global__ __launch_bounds__(256) void loss_zero_kernel(uint16_t* p, int64_t n) {
@@ -764,9 +1052,9 @@ __global__ __launch_bounds__(256) void loss_zero_kernel(uint16_t* p, int64_t n) 
 }
 
 template <int NW, int TB, int KIND>
-void launch_gemm_seg(const LossGemm& a, hipStream_t st) {
+void launch_gemm_seg(const LossGemm2& a, hipStream_t st) {
   const dim3 grid(kGemmXcds * Grid<NW, TB>::SLOTS), block(NW * 64);
-  if (a.nseg == 1)
+  if (a.g[0].nseg == 1)
     hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, 1, KIND>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, kLossMaxSeg, KIND>), grid, block, 0, st, a);
@@ -774,7 +1062,7 @@ void launch_gemm_seg(const LossGemm& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_loss_gemm(const LossGemm& a, int kind, int tile, hipStream_t st) {
+hipError_t launch_loss_gemm(const LossGemm2& a, int kind, int tile, hipStream_t st) {
   if (tile == kLossTile) {
     if (kind == kLossLogits) launch_gemm_seg<8, kLossTile, kLossLogits>(a, st);
     else launch_gemm_seg<8, kLossTile, kLossOut>(a, st);
@@ -785,24 +1073,16 @@ hipError_t launch_loss_gemm(const LossGemm& a, int kind, int tile, hipStream_t s
   return hipGetLastError();
 }
 
-hipError_t launch_loss_pack(const LossPack2& a, int blocks, hipStream_t st) {
-  hipLaunchKernelGGL(loss_pack_kernel, dim3(blocks), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_loss_targets(const LossTargets& a, hipStream_t st) {
-  hipLaunchKernelGGL(loss_targets_kernel, dim3(unsigned((a.n_pad + 3) / 4)), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_loss_sum(const float* a, const float* b, int64_t n, float scale, const float* denom, float* out,
-                           hipStream_t st) {
-  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, a, b, n, scale, denom, out);
+hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st) {
+  hipLaunchKernelGGL(loss_prep_kernel, dim3(blocks), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st) {
-  hipLaunchKernelGGL(loss_rows_kernel, dim3(a.rows_pad / 32), dim3(1024), 0, st, a);
+  const int per = loss_rows_per_block(a.rows_pad);
+  const dim3 grid(unsigned(a.rows_pad / per + (a.extra ? 1 : 0)));
+  if (per == 4) hipLaunchKernelGGL(loss_rows_kernel<4>, grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL(loss_rows_kernel<32>, grid, dim3(1024), 0, st, a);
   return hipGetLastError();
 }
 
@@ -816,11 +1096,31 @@ hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st) {
 }
 
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st) {
+  if (tile == 0) {
+    const int64_t quads = int64_t(a.rows) * ((a.cols + 3) / 4);
+    hipLaunchKernelGGL(loss_join_rows_kernel, dim3(unsigned((quads + 255) / 256)), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
   const dim3 grid(unsigned(a.tiles) * unsigned(tile * tile / 1024));
   if (tile == kLossTile)
     hipLaunchKernelGGL((loss_join_kernel<8, kLossTile>), grid, dim3(256), 0, st, a);
   else
     hipLaunchKernelGGL((loss_join_kernel<4, kLossTileSmall>), grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int KIND>
+void launch_stream(const LossStream& a, int mi, hipStream_t st) {
+  const int64_t items = int64_t(a.tiles) * a.splits;
+  const dim3 grid(unsigned(items < 256 ? items : 256)), block(512);
+  if (mi == 1) hipLaunchKernelGGL((loss_stream_kernel<1, KIND>), grid, block, 0, st, a);
+  else if (mi == 2) hipLaunchKernelGGL((loss_stream_kernel<2, KIND>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((loss_stream_kernel<4, KIND>), grid, block, 0, st, a);
+}
+
+hipError_t launch_loss_stream(const LossStream& a, int mi, int kind, hipStream_t st) {
+  if (kind == kLossLogits) launch_stream<kLossLogits>(a, mi, st);
+  else launch_stream<kLossOut>(a, mi, st);
   return hipGetLastError();
 }
 

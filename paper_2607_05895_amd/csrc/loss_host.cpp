@@ -1,15 +1,16 @@
 // Host side of the losses over a vocabulary: argument checks, workspace plan and launch sequence (all on the caller's
 // stream, descriptors as kernel arguments).
 //
-//   targets   ids, weights and entropy per token in one form; with MEAN the sum of the counted tokens' weights
-//   pack      x (this chunk's rows) and w as panel-blocked bf16, and transposed where a gradient reads them so
-//   per chunk of rows:
+//   per chunk of rows of x (usually one):
+//     prep    the labels in one form (first chunk); x's rows and (first chunk) w as panel-blocked bf16, and transposed where a
+//             gradient reads them so
 //     logits  z = x w^T: per row and 64 columns the softmax partials, the targets' logits and (for gradients) the logits
-//     rows    the partials joined: loss, and the factor of the row's gradient
+//     rows    the partials joined: loss, and the weight of the row's gradient; with MEAN (first chunk) the weights' sum; the
+//             last workgroup of all adds up the loss
 //     grad    dz, in both layouts
 //     dx      dz w            (K ranges and their join where there are few tiles)
-//     dw      dz^T x          (added to the earlier chunks' sum, held in fp32)
-//   loss      the sum over the tokens
+//     dw      dz^T x          (added to the earlier chunks' sum, held in fp32; in one launch with dx where both are small)
+// For a few tokens and bf16 the logits and dx read w as it lies instead of a packed copy.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -44,19 +45,25 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 struct Gemm {
   int tile = 0, tm = 0, tn = 0, splits = 1, kper = 0, nk = 0;
+  int64_t items() const { return int64_t(tm) * tn * splits; }
 };
 
 struct Plan {
   bool f32 = false, grads = false;
+  int stream = 0;               // rows / 32 of the products that read w as it lies, or 0
   int parts = 1, nseg = 1;
   int64_t n = 0, v = 0, h = 0, k = 1;
-  int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0, groups = 0;
+  int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0;
+  int group = kLossGroup;       // columns of a softmax partial
   Gemm logits, dx, dw;
   // offsets
-  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, row = 0, zt = 0, gm = 0, gs = 0;
+  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, counter = 0, row = 0, zt = 0, gm = 0, gs = 0;
   size_t xb = 0, xt = 0, wb = 0, wt = 0, codes = 0, z32 = 0, dz_t = 0, part = 0, acc = 0;
   size_t bytes = 0;
 };
+
+// Most tokens whose products read w as it lies, and the fewest ids.
+constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
 
 // Tile and K ranges of one product of M x N with K steps: the choice whose rounds of tiles over the chip's workgroups take
 // least, a step of a 256 x 256 tile taken as 1, of two 128 x 128 tiles on one CU as 0.6, a tile's start and epilogue as 12 steps and
@@ -121,20 +128,40 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.h = a->h;
   p.k = k;
   p.vp = up(p.v, 256);
-  p.hk = up(p.h, 32);
+  p.hk = up(p.h, 64);
   p.hp = up(p.h, 256);
-  p.groups = (p.v + kLossGroup - 1) / kLossGroup;
-  p.n_pad = up(std::max<int64_t>(p.n, 1), 256);
-  int64_t most = kMaxChunk;
-  if (p.grads) most = std::min(most, std::max<int64_t>(256, kLogitBytes / (2 * p.vp) / 256 * 256));
-  if (a->chunk_rows > 0) most = std::min(most, up(a->chunk_rows, 256));
-  p.chunk = std::min(p.n_pad, most);
-  p.logits = choose(p.chunk, p.v, p.nseg * p.hk / 32, false);
-  p.logits.nk = int(p.hk / 32);
-  const int64_t vsteps = up(p.v, 32) / 32;
-  if (a->dx) {
-    p.dx = choose(p.chunk, p.h, p.nseg * vsteps, true);
-    p.dx.nk = int(vsteps);
+  if (!p.f32 && p.n > 0 && p.n <= kStreamTokens && p.h % 8 == 0 && p.v >= kStreamIds) {
+    p.stream = p.n <= 32 ? 1 : p.n <= 64 ? 2 : 4;
+    p.group = 32;
+    p.chunk = p.n_pad = 32 * p.stream;
+  } else {
+    p.n_pad = up(std::max<int64_t>(p.n, 1), 256);
+    int64_t most = kMaxChunk;
+    if (p.grads) most = std::min(most, std::max<int64_t>(256, kLogitBytes / (2 * p.vp) / 256 * 256));
+    if (a->chunk_rows > 0) most = std::min(most, up(a->chunk_rows, 256));
+    p.chunk = std::min(p.n_pad, most);
+  }
+  const int64_t vsteps = up(p.v, 32) / 32, groups = (p.vp + p.group - 1) / p.group;
+  size_t part = 0;
+  if (p.stream) {
+    if (a->dx) {
+      // a workgroup per CU, in ranges of at least eight steps
+      const int64_t steps = up(p.v, 64) / 64, tiles = p.hp / 256;
+      const int64_t splits = std::max<int64_t>(1, std::min(steps / 8, (256 + tiles - 1) / tiles));
+      p.dx.nk = int(steps);
+      p.dx.tn = int(tiles);
+      p.dx.kper = int((steps + splits - 1) / splits);
+      p.dx.splits = int((steps + p.dx.kper - 1) / p.dx.kper);
+      part = size_t(p.dx.splits) * size_t(p.chunk * p.hp) * 4;
+    }
+  } else {
+    p.logits = choose(p.chunk, p.v, p.nseg * p.hk / 32, false);
+    p.logits.nk = int(p.hk / 32);
+    if (a->dx) {
+      p.dx = choose(p.chunk, p.h, p.nseg * vsteps, true);
+      p.dx.nk = int(vsteps);
+      if (p.dx.splits > 1) part = size_t(p.dx.items()) * size_t(p.dx.tile) * p.dx.tile * 4;
+    }
   }
   if (a->dw) p.dw = choose(p.v, p.h, p.nseg * p.chunk / 32, false);
   size_t o = 0;
@@ -150,21 +177,22 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.on = take(p.n_pad * 4);
   p.weighted = take(p.n_pad * 4);
   p.denom = take(4);
+  p.counter = take(4);
   p.row = take(p.chunk * 16);
   p.zt = take(p.chunk * k * 4);
-  p.gm = take((p.vp / kLossGroup) * p.chunk * 4);
-  p.gs = take((p.vp / kLossGroup) * p.chunk * 4);
+  p.gm = take(groups * p.chunk * 4);
+  p.gs = take(groups * p.chunk * 4);
   p.xb = take(p.chunk * p.hk * es);
-  p.wb = take(p.vp * p.hk * es);
+  if (!p.stream) p.wb = take(p.vp * p.hk * es);
   if (a->dw) p.xt = take(p.hp * p.chunk * es);
-  if (a->dx) p.wt = take(p.hp * p.vp * es);
+  if (a->dx && !p.stream) p.wt = take(p.hp * p.vp * es);
   if (p.grads) {
     p.codes = take(p.chunk * p.vp * es);
     if (p.f32) p.z32 = take(p.chunk * p.vp * 4);
   }
   if (a->dw) p.dz_t = take(p.vp * p.chunk * es);
-  if (p.dx.splits > 1) p.part = take(int64_t(p.dx.tm) * p.dx.tn * p.dx.splits * p.dx.tile * p.dx.tile * 4);
-  if (a->dw && p.chunk < p.n) p.acc = take(int64_t(p.dw.tm) * p.dw.tn * p.dw.tile * p.dw.tile * 4);
+  p.part = take(int64_t(part));
+  if (a->dw && p.chunk < p.n) p.acc = take(p.dw.items() * p.dw.tile * p.dw.tile * 4);
   p.bytes = o;
   return p;
 }
@@ -198,27 +226,15 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     return MFSDP_OK;
   }
   const float inv_t = float(1.0 / l.temperature), factor = float(a->scale / l.temperature);
-  LossTargets t{};
-  t.ids = l.ids;
-  t.logits = l.logits;
-  t.id64 = l.id_bytes == 8;
-  t.logits_bf16 = l.logit_dtype == MFSDP_BF16;
-  t.k = int32_t(k);
-  t.n = p.n;
-  t.n_pad = p.n_pad;
-  t.v = p.v;
-  t.ignore = l.ignore;
-  t.inv_t = inv_t;
-  t.id = reinterpret_cast<int32_t*>(ws + p.id);
-  t.q = f32p(p.q);
-  t.ent = f32p(p.ent);
-  t.on = f32p(p.on);
-  LOSS_TRY(launch_loss_targets(t, st), "targets launch");
-  float* denom = nullptr;
-  if (a->reduction == MFSDP_MEAN) {
-    denom = f32p(p.denom);
-    LOSS_TRY(launch_loss_sum(t.on, a->token_weight, p.n, 1.0f, nullptr, denom, st), "weight sum launch");
-  }
+  float* const denom = a->reduction == MFSDP_MEAN ? f32p(p.denom) : nullptr;
+  int32_t* const counter = reinterpret_cast<int32_t*>(ws + p.counter);
+  LossPrep prep{};
+  prep.l = LossLabels{l.ids, l.logits, l.id_bytes == 8, l.logit_dtype == MFSDP_BF16, int32_t(k), p.n, p.v, l.ignore, inv_t};
+  prep.n_pad = p.n_pad;
+  prep.id = reinterpret_cast<int32_t*>(ws + p.id);
+  prep.q = f32p(p.q);
+  prep.ent = f32p(p.ent);
+  prep.on = f32p(p.on);
 
   const int64_t xpart = p.chunk * p.hk, xtpart = p.hp * p.chunk, wpart = p.vp * p.hk, wtpart = p.hp * p.vp;
   const int64_t dzpart = p.chunk * p.vp;
@@ -242,13 +258,24 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     m.tn = g.tn;
     return m;
   };
+  int rows_blocks = denom ? 1 : 0;  // workgroups of all rows launches
   for (int64_t r0 = 0; r0 < p.n; r0 += p.chunk) {
-    const int64_t rows = std::min(p.chunk, p.n - r0), rows_pad = up(rows, 256);
-    LossPack2 pk{};
-    int blocks = 0;
+    const int rows_pad = int(up(std::min(p.chunk, p.n - r0), p.stream ? p.chunk : 256));
+    rows_blocks += rows_pad / loss_rows_per_block(rows_pad);
+  }
+  for (int64_t r0 = 0; r0 < p.n; r0 += p.chunk) {
+    const int64_t rows = std::min(p.chunk, p.n - r0), rows_pad = up(rows, p.stream ? p.chunk : 256);
+    const bool first = r0 == 0, last = r0 + p.chunk >= p.n;
+    const int32_t* ids = prep.id + r0 * k;
+    const float* q = prep.q + r0 * k;
+
+    prep.label_blocks = first ? int((p.n_pad + 3) / 4) : 0;
+    prep.counter = first ? counter : nullptr;
+    prep.packs = 0;
+    int blocks = prep.label_blocks;
     auto pack = [&](const void* src, int64_t R, int64_t rpad, size_t dst, int64_t part, bool with_t, size_t dst_t,
-                    int64_t ldt, int64_t tpart, const float* on) {
-      LossPack& d = pk.d[pk.count++];
+                    int64_t ldt, int64_t tpart, int64_t label_row) {
+      LossPack& d = prep.d[prep.packs++];
       d.src = src;
       d.R = R;
       d.C = p.h;
@@ -258,123 +285,188 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       d.dst_t = with_t ? u16p(dst_t) : nullptr;
       d.ldt = ldt;
       d.dst_t_part = tpart;
-      d.rows = rpad;
       d.cols = p.hp;
-      d.row_on = on;
+      d.label_row = label_row;
       d.blocks_begin = blocks;
       d.bf16 = !p.f32;
       blocks += int(rpad / 32 * (p.hp / 256));
     };
     pack(static_cast<const uint8_t*>(a->x) + r0 * p.h * es, rows, rows_pad, p.xb, xpart, a->dw != nullptr, p.xt, p.chunk,
-         xtpart, t.on + r0);
-    if (r0 == 0) pack(a->w, p.v, p.vp, p.wb, wpart, a->dx != nullptr, p.wt, p.vp, wtpart, nullptr);
-    LOSS_TRY(launch_loss_pack(pk, blocks, st), "pack launch");
+         xtpart, r0);
+    if (first && !p.stream) pack(a->w, p.v, p.vp, p.wb, wpart, a->dx != nullptr, p.wt, p.vp, wtpart, -1);
+    LOSS_TRY(launch_loss_prep(prep, blocks, st), "prep launch");
 
-    LossGemm z = product(p.logits, p.xb, p.hk, xpart, p.wb, p.hk, wpart, p.logits.nk);
-    z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
-    z.rows = int(rows);
-    z.cols = int(p.v);
-    z.inv_t = inv_t;
-    z.gm = f32p(p.gm);
-    z.gs = f32p(p.gs);
-    z.ldr = p.chunk;
-    z.ids = t.id + r0 * k;
-    z.zt = f32p(p.zt);
-    z.k = int32_t(k);
-    z.ldc = p.vp;
-    if (p.grads && p.f32) z.logits = f32p(p.z32);
-    if (p.grads && !p.f32) z.codes = u16p(p.codes);
-    LOSS_TRY(launch_loss_gemm(z, kLossLogits, p.logits.tile, st), "logits launch");
+    if (p.stream) {
+      LossStream z{};
+      z.P = u16p(p.xb);
+      z.w = static_cast<const uint16_t*>(a->w);
+      z.ldp = p.hk;
+      z.v = p.v;
+      z.h = p.h;
+      z.nk = int(p.hk / 64);
+      z.tiles = int(p.vp / 256);
+      z.splits = 1;
+      z.kper = z.nk;
+      z.inv_t = inv_t;
+      z.gm = f32p(p.gm);
+      z.gs = f32p(p.gs);
+      z.ldr = p.chunk;
+      z.ids = ids;
+      z.zt = f32p(p.zt);
+      z.k = int32_t(k);
+      z.codes = p.grads ? u16p(p.codes) : nullptr;
+      z.ldc = p.vp;
+      LOSS_TRY(launch_loss_stream(z, p.stream, kLossLogits, st), "logits launch");
+    } else {
+      LossGemm2 zz{};
+      LossGemm& z = zz.g[0];
+      z = product(p.logits, p.xb, p.hk, xpart, p.wb, p.hk, wpart, p.logits.nk);
+      zz.count = 1;
+      z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
+      z.rows = int(rows);
+      z.cols = int(p.v);
+      z.inv_t = inv_t;
+      z.gm = f32p(p.gm);
+      z.gs = f32p(p.gs);
+      z.ldr = p.chunk;
+      z.ids = ids;
+      z.zt = f32p(p.zt);
+      z.k = int32_t(k);
+      z.ldc = p.vp;
+      if (p.grads && p.f32) z.logits = f32p(p.z32);
+      if (p.grads && !p.f32) z.codes = u16p(p.codes);
+      LOSS_TRY(launch_loss_gemm(zz, kLossLogits, p.logits.tile, st), "logits launch");
+    }
 
     LossRows rw{};
-    rw.gm = z.gm;
-    rw.gs = z.gs;
+    rw.gm = f32p(p.gm);
+    rw.gs = f32p(p.gs);
     rw.ldr = p.chunk;
-    rw.groups = int(p.groups);
+    rw.groups = int((p.v + p.group - 1) / p.group);
     rw.rows = int(rows);
     rw.rows_pad = int(rows_pad);
     rw.k = int32_t(k);
-    rw.id = z.ids;
-    rw.q = t.q + r0 * k;
-    rw.ent = t.ent + r0;
-    rw.on = t.on + r0;
+    rw.id = ids;
+    rw.q = q;
+    rw.ent = prep.ent + r0;
+    rw.on = prep.on + r0;
     rw.weight = a->token_weight ? a->token_weight + r0 : nullptr;
-    rw.zt = z.zt;
+    rw.zt = f32p(p.zt);
     rw.z_loss = float(l.z_loss);
     rw.row = reinterpret_cast<float4*>(ws + p.row);
     rw.token_loss = a->token_loss ? a->token_loss + r0 : nullptr;
     rw.lse = a->lse ? a->lse + r0 : nullptr;
     rw.weighted = f32p(p.weighted) + r0;
+    rw.n = p.n;
+    rw.all_on = prep.on;
+    rw.all_weight = a->token_weight;
+    rw.all_weighted = f32p(p.weighted);
+    rw.denom = denom;
+    rw.denom_in = denom;
+    rw.loss = a->loss;
+    rw.scale = float(a->scale);
+    rw.extra = first && denom;
+    rw.last = last ? rows_blocks : 0;
+    rw.counter = counter;
     LOSS_TRY(launch_loss_rows(rw, st), "rows launch");
     if (!p.grads) continue;
 
     LossGrad gr{};
-    gr.codes = z.codes;
-    gr.logits = z.logits;
+    gr.codes = p.f32 ? nullptr : u16p(p.codes);
+    gr.logits = p.f32 ? f32p(p.z32) : nullptr;
     gr.ldc = p.vp;
     gr.dz = u16p(p.codes);
     gr.dz_t = a->dw ? u16p(p.dz_t) : nullptr;
     gr.dz_part = dzpart;
     gr.dz_t_part = dzpart;
     gr.ldt = p.chunk;
-    gr.gm = z.gm;
+    gr.gm = rw.gm;
     gr.ldr = p.chunk;
     gr.row = rw.row;
-    gr.id = z.ids;
-    gr.q = rw.q;
-    gr.zt = z.zt;
+    gr.id = ids;
+    gr.q = q;
+    gr.zt = rw.zt;
     gr.k = int32_t(k);
     gr.rows = int(rows);
     gr.rows_pad = int(rows_pad);
     gr.v = int(p.v);
     gr.v_pad = int(p.vp);
+    gr.group_shift = p.group == 32 ? 5 : 6;
     LOSS_TRY(launch_loss_grad(gr, st), "gradient launch");
 
-    if (a->dx) {
-      LossGemm m = product(p.dx, p.codes, p.vp, dzpart, p.wt, p.vp, wtpart, p.dx.nk);
-      m.tm = int(up(rows, p.dx.tile) / p.dx.tile);
-      m.rows = int(rows);
-      m.cols = int(p.h);
-      m.out = static_cast<uint8_t*>(a->dx) + r0 * p.h * es;
-      m.ldo = p.h;
-      m.out_bf16 = !p.f32;
-      m.alpha = factor;
-      m.denom = denom;
-      if (m.splits > 1) m.part = f32p(p.part);
-      LOSS_TRY(launch_loss_gemm(m, kLossOut, p.dx.tile, st), "dx launch");
-      if (m.splits > 1) {
-        LossJoin j{};
-        j.part = m.part;
-        j.splits = m.splits;
-        j.tiles = m.tm * m.tn;
-        j.tm = m.tm;
-        j.tn = m.tn;
-        j.rows = m.rows;
-        j.cols = m.cols;
-        j.out_bf16 = m.out_bf16;
-        j.out = m.out;
-        j.ldo = m.ldo;
-        j.alpha = m.alpha;
-        j.denom = m.denom;
-        LOSS_TRY(launch_loss_join(j, p.dx.tile, st), "dx join launch");
-      }
+    LossGemm mx{}, mw{};
+    if (a->dx && !p.stream) {
+      mx = product(p.dx, p.codes, p.vp, dzpart, p.wt, p.vp, wtpart, p.dx.nk);
+      mx.tm = int(up(rows, p.dx.tile) / p.dx.tile);
+      mx.rows = int(rows);
+      mx.cols = int(p.h);
+      mx.out = static_cast<uint8_t*>(a->dx) + r0 * p.h * es;
+      mx.ldo = p.h;
+      mx.out_bf16 = !p.f32;
+      mx.alpha = factor;
+      mx.denom = denom;
+      if (mx.splits > 1) mx.part = f32p(p.part);
     }
     if (a->dw) {
-      LossGemm m = product(p.dw, p.dz_t, p.chunk, dzpart, p.xt, p.chunk, xtpart, int(up(rows, 32) / 32));
-      m.rows = int(p.v);
-      m.cols = int(p.h);
-      m.out = a->dw;
-      m.ldo = p.h;
-      m.out_bf16 = !p.f32;
-      m.alpha = factor;
-      m.denom = denom;
-      if (r0 > 0) m.prev = f32p(p.acc);
-      if (r0 + p.chunk < p.n) m.part = f32p(p.acc);
-      LOSS_TRY(launch_loss_gemm(m, kLossOut, p.dw.tile, st), "dw launch");
+      mw = product(p.dw, p.dz_t, p.chunk, dzpart, p.xt, p.chunk, xtpart, int(up(rows, 32) / 32));
+      mw.rows = int(p.v);
+      mw.cols = int(p.h);
+      mw.out = a->dw;
+      mw.ldo = p.h;
+      mw.out_bf16 = !p.f32;
+      mw.alpha = factor;
+      mw.denom = denom;
+      if (!first) mw.prev = f32p(p.acc);
+      if (!last) mw.part = f32p(p.acc);
+    }
+    LossGemm2 both{};
+    // one launch where the tiles of both fit the chip at once
+    const bool together = a->dx && a->dw && !p.stream && p.dx.tile == p.dw.tile &&
+                          p.dx.items() + p.dw.items() <= (p.dx.tile == kLossTile ? 256 : 512);
+    if (a->dx && p.stream) {
+      LossStream s{};
+      s.P = u16p(p.codes);
+      s.w = static_cast<const uint16_t*>(a->w);
+      s.ldp = p.vp;
+      s.v = p.v;
+      s.h = p.h;
+      s.nk = p.dx.nk;
+      s.tiles = p.dx.tn;
+      s.splits = p.dx.splits;
+      s.kper = p.dx.kper;
+      s.part = f32p(p.part);
+      s.ldo = p.hp;
+      LOSS_TRY(launch_loss_stream(s, p.stream, kLossOut, st), "dx launch");
+    } else if (a->dx) {
+      both.g[0] = mx;
+      both.g[1] = mw;
+      both.count = together ? 2 : 1;
+      LOSS_TRY(launch_loss_gemm(both, kLossOut, p.dx.tile, st), "dx launch");
+    }
+    if (a->dw && !together) {
+      both.g[0] = mw;
+      both.count = 1;
+      LOSS_TRY(launch_loss_gemm(both, kLossOut, p.dw.tile, st), "dw launch");
+    }
+    if (a->dx && (p.stream || mx.splits > 1)) {
+      LossJoin j{};
+      j.part = f32p(p.part);
+      j.splits = p.stream ? p.dx.splits : mx.splits;
+      j.tiles = mx.tm * mx.tn;
+      j.tm = mx.tm;
+      j.tn = mx.tn;
+      j.rows = int(rows);
+      j.cols = int(p.h);
+      j.out_bf16 = !p.f32;
+      j.stride = p.chunk * p.hp;
+      j.ldp = p.hp;
+      j.out = static_cast<uint8_t*>(a->dx) + r0 * p.h * es;
+      j.ldo = p.h;
+      j.alpha = factor;
+      j.denom = denom;
+      LOSS_TRY(launch_loss_join(j, p.stream ? 0 : p.dx.tile, st), "dx join launch");
     }
   }
-  if (a->loss)
-    LOSS_TRY(launch_loss_sum(f32p(p.weighted), nullptr, p.n, float(a->scale), denom, a->loss, st), "loss sum launch");
 #undef LOSS_TRY
   return MFSDP_OK;
 }

@@ -8,8 +8,8 @@
 // tensor is held in three bf16 parts, and a product runs over six pairs of parts, one K segment each.
 //
 // Between the logits and their gradient a chunk of bf16 inputs holds each logit in 16 bits: the distance
-// from the largest of its row in its 64 columns, in steps of 2^-10 of a factor of two. That is a relative error of p of
-// at most 2^-11 ln 2 = 3.4e-4, a sixth of the rounding of dz to bf16 that follows, at half the bytes of fp32, and
+// from the largest of its row in its 64 columns, in steps of 64 / 65535 of a factor of two. That is a relative error of p of
+// at most half a step times ln 2 = 3.4e-4, a sixth of the rounding of dz to bf16 that follows, at half the bytes of fp32, and
 // the bf16 dz then takes the codes' place. (Below 2^-64 of that largest one p is taken as 0.) What p - q loses where they
 // are near is not lost here: the logits of the targets are kept in fp32. For fp32 inputs the logits are kept in fp32.
 #pragma once
@@ -23,10 +23,10 @@ namespace mfsdp {
 
 constexpr int kLossTile = 256;       // output tile of the products (kLossTileSmall for launches with few tiles)
 constexpr int kLossTileSmall = 128;
-constexpr int kLossGroup = 64;       // columns of one softmax partial
+constexpr int kLossGroup = 64;       // columns of one softmax partial (of the products for a few tokens: 32)
 constexpr int kLossMaxSeg = 6;
 constexpr int kLossMaxTop = 256;     // most teacher logits a token
-constexpr float kLossCodeStep = 1024.0f;  // codes per factor of two
+constexpr float kLossOctaves = 64.0f;  // factors of two that the 16-bit codes of the logits span
 
 // One NT product over panel-blocked operands: tiles of P Q^T, K in nseg segments (part pairs) of nk steps of 32, cut
 // into `splits` ranges of kper steps.
@@ -57,6 +57,39 @@ struct LossGemm {
   const float* denom;
 };
 
+// Up to two products of one launch (the second one's tiles follow the first one's).
+struct LossGemm2 {
+  LossGemm g[2];
+  int32_t count;
+};
+
+// Products for a few tokens (at most 32 MI), where reading w counts: w is read as it lies, once, with no packed copy.
+//   logits: tiles of 256 ids, K = h in steps of 64;  dx: tiles of 256 columns of h, K = v in steps of 64, cut into `splits` ranges of
+//   kper steps, whose fp32 results lie row-major (32 MI x ldo) one after another in part.
+struct LossStream {
+  const uint16_t *P, *w;     // P: x, or dz; panel blocked with ldp columns
+  int64_t ldp, v, h;
+  int32_t nk, tiles, splits, kper;
+  float inv_t;
+  float *gm, *gs;            // per row and 32 columns, [group][ldr]
+  int64_t ldr;
+  const int32_t* ids;
+  float* zt;
+  int32_t k;
+  uint16_t* codes;
+  int64_t ldc;
+  float* part;
+  int64_t ldo;
+};
+
+// Labels as the caller has them: n x k ids; logits: the teacher's (null: hard labels, of which `ignore` marks none).
+struct LossLabels {
+  const void *ids, *logits;
+  int32_t id64, logits_bf16, k;
+  int64_t n, v, ignore;
+  float inv_t;
+};
+
 // Panel-blocked bf16 copies of a row-major R x C matrix: as it is (dst, ldn columns) and transposed (dst_t, ldt columns),
 // in `parts` parts (1: bf16 source; 3: fp32 source) that lie dst_part (dst_t_part) elements apart.
 struct LossPack {
@@ -64,28 +97,27 @@ struct LossPack {
   int64_t R, C;
   uint16_t *dst, *dst_t;
   int64_t ldn, ldt, dst_part, dst_t_part;
-  int64_t rows, cols;          // padded extent to write (multiples of 32 and of 256)
-  const float* row_on;         // rows whose entry is 0 are written as zeros (whatever they hold); null: all
+  int64_t cols;                // padded columns (a multiple of 256)
+  int64_t label_row;           // the label of row 0 (rows whose token does not count are written as zeros), or -1: all rows
   int32_t blocks_begin, bf16;  // first workgroup
 };
-struct LossPack2 {
-  LossPack d[2];
-  int32_t count;
-};
 
-// Targets in one form: per token k ids with weights q that add up to 1 (0 and -1: none), the sum of q log q, and whether
-// the token counts (on: 1, 0, or NaN for an id outside the vocabulary).
-struct LossTargets {
-  const void *ids, *logits;    // n x k; logits: the teacher's (null: hard labels)
-  int32_t id64, logits_bf16, k;
-  int64_t n, n_pad, v, ignore;
-  float inv_t;
-  int32_t* id;
+// The first launch: the labels in one form (per token k ids with weights q that add up to 1, -1 and 0 for none; the sum of
+// q log q; on: whether the token counts, 1, 0, or NaN for an id outside the vocabulary), the packed operands, and a
+// counter of the rows launches' finished workgroups set to 0.
+struct LossPrep {
+  LossLabels l;
+  int64_t n_pad;
+  int32_t label_blocks;        // workgroups of four tokens each; the packs' workgroups follow
+  int32_t *id, *counter;
   float *q, *ent, *on;
+  LossPack d[2];
+  int32_t packs;
 };
 
 // Per row of a chunk: the row's softmax (largest logit M, sum s of the others' exp relative to it), its loss and its weight
-// in the gradient.
+// in the gradient. The first chunk's launch has one more workgroup, for denom (the counted tokens' weights' sum), and the
+// workgroup that ends last of all launches adds up the loss.
 struct LossRows {
   const float *gm, *gs;
   int64_t ldr;
@@ -96,10 +128,19 @@ struct LossRows {
   float4* row;                 // {M, s, weight, 2 z_loss lse}
   float *token_loss, *lse;     // optional
   float* weighted;             // weight x loss
+  // all tokens'
+  int64_t n;
+  const float *all_on, *all_weight, *all_weighted;
+  float *denom, *loss;         // optional; denom: of this launch's extra workgroup
+  const float* denom_in;       // null: 1
+  float scale;
+  int32_t extra, last;         // an extra workgroup; workgroups of all launches where this is the last one (else 0)
+  int32_t* counter;
 };
 
 // dz of a chunk, without the factor scale / (T D) common to all tokens (which the products apply: rounded with it, the
-// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place and transposed, or fp32 logits -> three bf16 parts and their transposes.
+// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place and transposed, or fp32
+// logits -> three bf16 parts and their transposes.
 struct LossGrad {
   uint16_t* codes;
   const float* logits;
@@ -112,11 +153,15 @@ struct LossGrad {
   const int32_t* id;
   const float *q, *zt;
   int32_t k, rows, rows_pad, v, v_pad;
+  int32_t group_shift;         // log2 of the columns of one softmax partial
 };
 
+// out = alpha / denom times the sum of the K ranges' results in their order: tiles in accumulator order (tile > 0), or
+// row-major ones of `stride` elements (tile 0).
 struct LossJoin {
   const float* part;
   int32_t splits, tiles, tm, tn, rows, cols, out_bf16;
+  int64_t stride, ldp;
   void* out;
   int64_t ldo;
   float alpha;
@@ -124,16 +169,14 @@ struct LossJoin {
 };
 
 enum { kLossLogits = 0, kLossOut = 1 };
-hipError_t launch_loss_gemm(const LossGemm& a, int kind, int tile, hipStream_t st);
-hipError_t launch_loss_pack(const LossPack2& a, int blocks, hipStream_t st);
-hipError_t launch_loss_targets(const LossTargets& a, hipStream_t st);
-// out[0] = f(sum of a (times b where given) over n values), in a fixed order: mode 0 the sum times scale, 1 that over denom[0] (0
-// where denom is 0)
-hipError_t launch_loss_sum(const float* a, const float* b, int64_t n, float scale, const float* denom, float* out,
-                           hipStream_t st);
+hipError_t launch_loss_gemm(const LossGemm2& a, int kind, int tile, hipStream_t st);
+hipError_t launch_loss_stream(const LossStream& a, int mi, int kind, hipStream_t st);
+hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st);
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st);
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st);
 hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st);
+// Rows of one workgroup of the rows launch.
+constexpr int loss_rows_per_block(int rows_pad) { return rows_pad <= 256 ? 4 : 32; }
 
 }  // namespace mfsdp

@@ -129,7 +129,10 @@ def _check_loss(got, ref, tol_rel=2.0 ** -15):
 
 
 SHAPES = [(1, 1, 1), (1, 300, 64), (3, 64, 8), (7, 1003, 97), (64, 1000, 64), (255, 257, 33), (256, 256, 32),
-          (257, 513, 257), (130, 4100, 200), (600, 2049, 520)]
+          (257, 513, 257), (130, 4100, 200), (600, 2049, 520),
+          # few tokens on many ids: w is read as it lies
+          (1, 4096, 64), (31, 4100, 72), (32, 4111, 264), (33, 5003, 200), (64, 4097, 8), (100, 9001, 136), (128, 4351, 1000),
+          (17, 4500, 129)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -153,7 +156,8 @@ def test_xent_matches_the_oracle(n, v, h, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,v,h,k", [(1, 40, 16, 1), (5, 70, 24, 3), (33, 1003, 96, 5), (130, 600, 64, 64),
-                                     (257, 2100, 136, 65), (40, 300, 72, 256)])
+                                     (257, 2100, 136, 65), (40, 300, 72, 256), (20, 4500, 80, 7),
+                                     (1, 4500, 72, 3), (70, 4111, 104, 33), (128, 5000, 320, 4)])
 def test_distill_matches_the_oracle(n, v, h, k, dtype):
     rng = np.random.default_rng(n + v + h + k)
     x, w, x64, w64 = _inputs(rng, n, v, h, dtype)
