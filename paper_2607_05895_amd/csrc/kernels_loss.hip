@@ -624,7 +624,6 @@ __device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, 
 __global__ __launch_bounds__(256) void loss_prep_kernel(const LossPrep a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
   __shared__ int counts[32];
-  if (blockIdx.x == 0 && threadIdx.x == 0 && a.counter) *a.counter = 0;
   if (int(blockIdx.x) < a.label_blocks) {
     const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (r < a.n_pad) prep_labels(a, r);
@@ -661,7 +660,6 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
   constexpr int GS = 1024 / RPB;
   __shared__ float sm[GS][RPB + 1], ss[GS][RPB + 1];
   __shared__ double part[16];
-  __shared__ int last;
   const int blocks = a.rows_pad / RPB;
   if (int(blockIdx.x) == blocks) {  // (the extra workgroup)
     const double d = block_sum<1024>(a.all_on, a.all_weight, a.n, part);
@@ -716,16 +714,17 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
       }
     }
   }
-  if (!a.loss) return;
-  // the workgroup that ends last, of every chunk's launches, sees all the others' results
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(a.counter, 1) + 1 == a.last;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  const double t = block_sum<1024>(a.all_weighted, nullptr, a.n, part) * a.scale;
-  if (threadIdx.x == 0) a.loss[0] = float(!a.denom_in ? t : a.denom_in[0] != 0.0f ? t / a.denom_in[0] : t == t ? 0.0 : t);
+}
+
+// The loss of all tokens from their weighted losses, by one workgroup.
+template <int T>
+__device__ __forceinline__ void sum_loss(const LossTotal& a, double* part) {
+  const double t = block_sum<T>(a.weighted, nullptr, a.n, part) * a.scale;
+  if (threadIdx.x == 0) a.loss[0] = float(!a.denom ? t : a.denom[0] != 0.0f ? t / a.denom[0] : t == t ? 0.0 : t);
+}
+__global__ __launch_bounds__(1024) void loss_total_kernel(const LossTotal a) {
+  __shared__ double part[16];
+  sum_loss<1024>(a, part);
 }
 
 // One 32 x 256 tile of dz per workgroup of 256: from the logits to LDS, the targets' elements there from their fp32 logits,
@@ -736,6 +735,10 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   __shared__ float fix[F32 ? 32 * 256 : 1];
   lds_byte* tile = (lds_byte*)smem;
   const int tc = a.v_pad / 256;
+  if (int64_t(blockIdx.x) == int64_t(a.rows_pad / 32) * tc) {  // (one more workgroup, for the loss)
+    sum_loss<256>(a.total, (double*)smem);
+    return;
+  }
   const int64_t r0 = int64_t(blockIdx.x / tc) * 32, c0 = int64_t(blockIdx.x % tc) * 256;
   const int t = threadIdx.x, ln = t & 63, w = t >> 6;
   // chunk (row, 8 columns) it of a thread: bf16 as its 1 KiB block lies (lane: row lane / 4, chunk lane % 4); fp32
@@ -1080,14 +1083,19 @@ hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st) {
 
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st) {
   const int per = loss_rows_per_block(a.rows_pad);
-  const dim3 grid(unsigned(a.rows_pad / per + (a.extra ? 1 : 0)));
+  const dim3 grid(unsigned(a.rows_pad / per + (a.denom ? 1 : 0)));
   if (per == 4) hipLaunchKernelGGL(loss_rows_kernel<4>, grid, dim3(1024), 0, st, a);
   else hipLaunchKernelGGL(loss_rows_kernel<32>, grid, dim3(1024), 0, st, a);
   return hipGetLastError();
 }
 
+hipError_t launch_loss_total(const LossTotal& a, hipStream_t st) {
+  hipLaunchKernelGGL(loss_total_kernel, dim3(1), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st) {
-  const dim3 grid(unsigned(a.rows_pad / 32) * unsigned(a.v_pad / 256));
+  const dim3 grid(unsigned(a.rows_pad / 32) * unsigned(a.v_pad / 256) + (a.total.loss ? 1u : 0u));
   if (a.logits)
     hipLaunchKernelGGL(loss_grad_kernel<true>, grid, dim3(256), 0, st, a);
   else

@@ -5,9 +5,9 @@
 //     prep    the labels in one form (first chunk); x's rows and (first chunk) w as panel-blocked bf16, and transposed where a
 //             gradient reads them so
 //     logits  z = x w^T: per row and 64 columns the softmax partials, the targets' logits and (for gradients) the logits
-//     rows    the partials joined: loss, and the weight of the row's gradient; with MEAN (first chunk) the weights' sum; the
-//             last workgroup of all adds up the loss
-//     grad    dz, in both layouts
+//     rows    the partials joined: the tokens' losses, and the weights of their gradients; with MEAN (first chunk) the weights'
+//             sum
+//     grad    dz, in both layouts; (last chunk) the loss
 //     dx      dz w            (K ranges and their join where there are few tiles)
 //     dw      dz^T x          (added to the earlier chunks' sum, held in fp32; in one launch with dx where both are small)
 // For a few tokens and bf16 the logits and dx read w as it lies instead of a packed copy.
@@ -57,7 +57,7 @@ struct Plan {
   int group = kLossGroup;       // columns of a softmax partial
   Gemm logits, dx, dw;
   // offsets
-  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, counter = 0, row = 0, zt = 0, gm = 0, gs = 0;
+  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, row = 0, zt = 0, gm = 0, gs = 0;
   size_t xb = 0, xt = 0, wb = 0, wt = 0, codes = 0, z32 = 0, dz_t = 0, part = 0, acc = 0;
   size_t bytes = 0;
 };
@@ -177,7 +177,6 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.on = take(p.n_pad * 4);
   p.weighted = take(p.n_pad * 4);
   p.denom = take(4);
-  p.counter = take(4);
   p.row = take(p.chunk * 16);
   p.zt = take(p.chunk * k * 4);
   p.gm = take(groups * p.chunk * 4);
@@ -227,7 +226,6 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
   }
   const float inv_t = float(1.0 / l.temperature), factor = float(a->scale / l.temperature);
   float* const denom = a->reduction == MFSDP_MEAN ? f32p(p.denom) : nullptr;
-  int32_t* const counter = reinterpret_cast<int32_t*>(ws + p.counter);
   LossPrep prep{};
   prep.l = LossLabels{l.ids, l.logits, l.id_bytes == 8, l.logit_dtype == MFSDP_BF16, int32_t(k), p.n, p.v, l.ignore, inv_t};
   prep.n_pad = p.n_pad;
@@ -258,11 +256,6 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     m.tn = g.tn;
     return m;
   };
-  int rows_blocks = denom ? 1 : 0;  // workgroups of all rows launches
-  for (int64_t r0 = 0; r0 < p.n; r0 += p.chunk) {
-    const int rows_pad = int(up(std::min(p.chunk, p.n - r0), p.stream ? p.chunk : 256));
-    rows_blocks += rows_pad / loss_rows_per_block(rows_pad);
-  }
   for (int64_t r0 = 0; r0 < p.n; r0 += p.chunk) {
     const int64_t rows = std::min(p.chunk, p.n - r0), rows_pad = up(rows, p.stream ? p.chunk : 256);
     const bool first = r0 == 0, last = r0 + p.chunk >= p.n;
@@ -270,7 +263,6 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     const float* q = prep.q + r0 * k;
 
     prep.label_blocks = first ? int((p.n_pad + 3) / 4) : 0;
-    prep.counter = first ? counter : nullptr;
     prep.packs = 0;
     int blocks = prep.label_blocks;
     auto pack = [&](const void* src, int64_t R, int64_t rpad, size_t dst, int64_t part, bool with_t, size_t dst_t,
@@ -360,16 +352,13 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     rw.n = p.n;
     rw.all_on = prep.on;
     rw.all_weight = a->token_weight;
-    rw.all_weighted = f32p(p.weighted);
-    rw.denom = denom;
-    rw.denom_in = denom;
-    rw.loss = a->loss;
-    rw.scale = float(a->scale);
-    rw.extra = first && denom;
-    rw.last = last ? rows_blocks : 0;
-    rw.counter = counter;
+    rw.denom = first ? denom : nullptr;
     LOSS_TRY(launch_loss_rows(rw, st), "rows launch");
-    if (!p.grads) continue;
+    const LossTotal total{f32p(p.weighted), denom, p.n, float(a->scale), last ? a->loss : nullptr};
+    if (!p.grads) {
+      if (total.loss) LOSS_TRY(launch_loss_total(total, st), "loss sum launch");
+      continue;
+    }
 
     LossGrad gr{};
     gr.codes = p.f32 ? nullptr : u16p(p.codes);
@@ -392,6 +381,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     gr.v = int(p.v);
     gr.v_pad = int(p.vp);
     gr.group_shift = p.group == 32 ? 5 : 6;
+    gr.total = total;
     LOSS_TRY(launch_loss_grad(gr, st), "gradient launch");
 
     LossGemm mx{}, mw{};

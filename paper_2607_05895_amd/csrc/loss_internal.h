@@ -103,21 +103,28 @@ struct LossPack {
 };
 
 // The first launch: the labels in one form (per token k ids with weights q that add up to 1, -1 and 0 for none; the sum of
-// q log q; on: whether the token counts, 1, 0, or NaN for an id outside the vocabulary), the packed operands, and a
-// counter of the rows launches' finished workgroups set to 0.
+// q log q; on: whether the token counts, 1, 0, or NaN for an id outside the vocabulary), and the packed operands.
 struct LossPrep {
   LossLabels l;
   int64_t n_pad;
   int32_t label_blocks;        // workgroups of four tokens each; the packs' workgroups follow
-  int32_t *id, *counter;
+  int32_t* id;
   float *q, *ent, *on;
   LossPack d[2];
   int32_t packs;
 };
 
+// The loss of all tokens: scale / denom[0] (denom null: 1; 0: loss 0) times the sum of their weighted losses.
+struct LossTotal {
+  const float *weighted, *denom;
+  int64_t n;
+  float scale;
+  float* loss;
+};
+
 // Per row of a chunk: the row's softmax (largest logit M, sum s of the others' exp relative to it), its loss and its weight
-// in the gradient. The first chunk's launch has one more workgroup, for denom (the counted tokens' weights' sum), and the
-// workgroup that ends last of all launches adds up the loss.
+// in the gradient. The first chunk's launch may have one more workgroup, for denom (the sum of the weights of the tokens that
+// count).
 struct LossRows {
   const float *gm, *gs;
   int64_t ldr;
@@ -128,14 +135,9 @@ struct LossRows {
   float4* row;                 // {M, s, weight, 2 z_loss lse}
   float *token_loss, *lse;     // optional
   float* weighted;             // weight x loss
-  // all tokens'
-  int64_t n;
-  const float *all_on, *all_weight, *all_weighted;
-  float *denom, *loss;         // optional; denom: of this launch's extra workgroup
-  const float* denom_in;       // null: 1
-  float scale;
-  int32_t extra, last;         // an extra workgroup; workgroups of all launches where this is the last one (else 0)
-  int32_t* counter;
+  int64_t n;                   // for denom: all tokens
+  const float *all_on, *all_weight;
+  float* denom;                // null: no such workgroup
 };
 
 // dz of a chunk, without the factor scale / (T D) common to all tokens (which the products apply: rounded with it, the
@@ -154,6 +156,7 @@ struct LossGrad {
   const float *q, *zt;
   int32_t k, rows, rows_pad, v, v_pad;
   int32_t group_shift;         // log2 of the columns of one softmax partial
+  LossTotal total;             // loss not null: summed by one more workgroup
 };
 
 // out = alpha / denom times the sum of the K ranges' results in their order: tiles in accumulator order (tile > 0), or
@@ -173,6 +176,7 @@ hipError_t launch_loss_gemm(const LossGemm2& a, int kind, int tile, hipStream_t 
 hipError_t launch_loss_stream(const LossStream& a, int mi, int kind, hipStream_t st);
 hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st);
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st);
+hipError_t launch_loss_total(const LossTotal& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st);
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st);
 hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st);
