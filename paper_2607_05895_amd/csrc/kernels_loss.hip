@@ -72,6 +72,16 @@ __device__ __forceinline__ uint32_t code2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(a, b));
 }
 
+// a lane's value joined with the other half wave's
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 struct Item {
   int p, bi, bj, k0, nk;  // problem, tile, K steps
 };
@@ -80,7 +90,7 @@ struct Item {
 // direct global->LDS loads of whole 1 KiB blocks by one wave of each SIMD, one barrier per K step of 32 inside its second
 // 16-wide slice, the next step's fragments read while the rest of that slice multiplies, and the next tile's first loads
 // issued before this tile's epilogue. Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
-// column); the order is arithmetic, so a launch needs no schedule in memory.
+// column) and taken from counters, so that long and short tiles (the K ranges of dx, the tiles of dw) share the chip evenly.
 template <int NW, int TB, int NSEG, int KIND>
 __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm2 b) {
   using G = Grid<NW, TB>;
@@ -89,15 +99,43 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / G::WN, wn = w % G::WN;
-  const int xcd = blockIdx.x % kGemmXcds, slot = blockIdx.x / kGemmXcds;
   const int first = b.g[0].tm * b.g[0].tn * b.g[0].splits;
   const int total = first + (KIND == kLossOut && b.count > 1 ? b.g[1].tm * b.g[1].tn * b.g[1].splits : 0);
-  const int per = min(G::SLOTS, (total + kGemmXcds - 1) / kGemmXcds);  // tiles of one group
-  if (slot >= per) return;
+  const int per = min(G::SLOTS, (total + kGemmXcds - 1) / kGemmXcds);  // items of one group
+  const int groups = (total + per - 1) / per;
 
-  auto item_at = [&](int g, Item& it) -> bool {
-    int i = g * per + slot;
-    if (i >= total) return false;
+  // Items are dealt in groups that run together on one XCD: group g belongs to XCD g % 8. A workgroup's first item is its place in
+  // its XCD's first group; the next ones come from a counter of its XCD or, once that has run out, of the XCD with the
+  // most items left. (One lane asks; -1: none left.)
+  const int home = blockIdx.x % kGemmXcds, place = blockIdx.x / kGemmXcds;
+  if (place >= per) return;
+  auto left_in = [&](int x, int taken) {  // XCD x's items beyond its first group that are not taken yet
+    const int ng = (groups - x + kGemmXcds - 1) / kGemmXcds;
+    return (ng - 1) * per - ((groups - 1) % kGemmXcds == x ? groups * per - total : 0) - taken;
+  };
+  bool home_out = false;
+  auto take = [&]() -> int {
+    gptr<int> q = (gptr<int>)b.queue;
+    for (int x = home;;) {
+      if (home_out) {
+        int most = 0;
+#pragma unroll
+        for (int y = 0; y < kGemmXcds; ++y) {
+          const int n = left_in(y, __hip_atomic_load(q + y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+          if (n > most) {
+            most = n;
+            x = y;
+          }
+        }
+        if (most == 0) return -1;
+      }
+      const int i = __hip_atomic_fetch_add(q + x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (left_in(x, i) > 0) return ((i / per + 1) * kGemmXcds + x) * per + i % per;
+      home_out = true;
+    }
+  };
+  auto item_at = [&](int i, Item& it) -> bool {
+    if (i < 0 || i >= total) return false;
     it.p = KIND == kLossOut && i >= first ? 1 : 0;
     const LossGemm& a = b.g[it.p];
     if (it.p) i -= first;
@@ -164,13 +202,20 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   const int slot1 = ((2 + fhalf) ^ swz(frow)) * 16;
   constexpr int NMF = MI * NI, NRD = MI + NI;  // MFMAs and fragment reads per 16-wide slice
 
-  int g = xcd;
   Item cur, nxt;
-  if (!item_at(g, cur)) return;
+  if (!item_at(home * per + place, cur)) return;
   if (issuer) prologue(cur);
+  // (the last stage is free whenever items are taken; the last wave asks: of eight waves it issues no loads to wait behind)
+  int* mail = reinterpret_cast<int*>(smem + (kStages - 1) * STAGE);
+  const bool asks = threadIdx.x == (NW - 1) * 64, queued = groups > kGemmXcds;
+  bool has_next = false;
+  if (queued) {
+    if (asks) mail[0] = take();
+    LOSS_WAIT_LGKM0();
+    __builtin_amdgcn_s_barrier();
+    has_next = item_at(__builtin_amdgcn_readfirstlane(mail[0]), nxt);
+  }
   while (true) {
-    g += kGemmXcds;
-    const bool has_next = item_at(g, nxt);
 
     f32x16_t acc[MI][NI];
 #pragma unroll
@@ -242,6 +287,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     LOSS_WAIT_VMCNT(0);
     __builtin_amdgcn_s_barrier();
     if (has_next && issuer) prologue(nxt);  // (leaves stage kStages - 1 to the epilogue)
+    int after = -1;  // the item after that: asked for here, needed at the epilogue's end
+    if (has_next && asks) after = take();
 
     // acc[mi][ni][4 gg + t] of a lane is element (row, column) of the wave's part with row = 32 mi + lane % 32,
     // column = 32 ni + 8 gg + 4 (lane / 32) + t.
@@ -273,6 +320,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
             for (int mi = 0; mi < MI; ++mi) acc[mi][e >> 4][e & 15] = -__builtin_inff();
           }
       }
+      float top[MI];
       static_for<MI>([&](auto mi_c) {
         constexpr int mi = decltype(mi_c)::value;
         const int row = row0 + mi * 32;
@@ -282,7 +330,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         float m = u[0];
 #pragma unroll
         for (int e = 1; e < 32; ++e) m = fmaxf(m, u[e]);
-        m = fmaxf(m, __shfl_xor(m, 32));
+        m = top[mi] = half_max(m);
         // Sum of the others' exp: the largest term itself is 1, and what is far below it must not vanish in that 1. A
         // term's fraction is the term, but 0 for a 1; how many ones there are (equal logits) is what the two sums differ by.
         float s = 0.0f, all = 0.0f;
@@ -292,9 +340,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           s += __builtin_amdgcn_fractf(x);
           all += x;
         }
-        float ones = __builtin_rintf(all - s);
-        s += __shfl_xor(s, 32);
-        ones += __shfl_xor(ones, 32);
+        const float ones = half_sum(__builtin_rintf(all - s));
+        s = half_sum(s);
         if (left > 0 && eh == 0) {
           const int64_t at = int64_t(c0 >> 6) * a.ldr + row;
           a.gm[at] = m * a.inv_t;
@@ -311,12 +358,12 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           }
         };
         target(id0[mi], 0);
-        for (int j = 1; j < a.k; j += 4) {
-          int id[4];
+        for (int j = 1; j < a.k; j += 16) {
+          int id[16];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) id[i] = j + i < a.k ? a.ids[int64_t(row) * a.k + j + i] : -1;
+          for (int i = 0; i < 16; ++i) id[i] = j + i < a.k ? *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j + i) : -1;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) target(id[i], j + i);
+          for (int i = 0; i < 16; ++i) target(id[i], j + i);
         }
         if (a.logits) {
           float* dst = a.logits + int64_t(row) * a.ldc + c0;
@@ -325,15 +372,19 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
             *(gptr<f32x4_t>)(dst + (p >> 2) * 32 + (p & 3) * 8 + eh * 4) =
                 f32x4_t{u[4 * p] * a.inv_t, u[4 * p + 1] * a.inv_t, u[4 * p + 2] * a.inv_t, u[4 * p + 3] * a.inv_t};
         }
-        if (a.codes) {
+      });
+      if (a.codes) {
+        static_for<MI>([&](auto mi_c) {
+          constexpr int mi = decltype(mi_c)::value;
           // round(65535 x) for x in [0, 1], clamped: x = 1 is kLossOctaves factors of two below the largest
-          const float C = -L * (1.0f / kLossOctaves);
+          const float C = -L * (1.0f / kLossOctaves), m = top[mi];
 #pragma unroll
-          for (int p = 0; p < 8; ++p)
+          for (int p = 0; p < 8; ++p) {
+            const f32x16_t& u = acc[mi][p >> 2];
+            const int o = 4 * (p & 3);
             *(lptr<u32x2>)(slab + wr_base + (p >> 2) * 1024 + ((((p & 3) ^ wsw) - wsw) << 4)) =
-                u32x2{code2((u[4 * p] - m) * C, (u[4 * p + 1] - m) * C), code2((u[4 * p + 2] - m) * C, (u[4 * p + 3] - m) * C)};
-        }
-        if (a.codes) {
+                u32x2{code2((u[o] - m) * C, (u[o + 1] - m) * C), code2((u[o + 2] - m) * C, (u[o + 3] - m) * C)};
+          }
           LOSS_WAIT_LGKM0();
           __builtin_amdgcn_s_barrier();
           const int rin = ln >> 2, ch = ln & 3;
@@ -345,8 +396,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
             *(gptr<u32x4>)(a.codes + blk_index(int64_t(cur.bi) * TB + dr, int64_t(cur.bj) * TB + cb * 32 + ch * 8, a.ldc)) = val;
           }
           __builtin_amdgcn_s_barrier();
-        }
-      });
+        });
+      }
     } else {
       const int i = (cur.bj * a.tm + cur.bi) * a.splits + cur.k0 / a.kper;  // tile and range
       const int64_t tile_at = int64_t(i) * (TB * TB) + (w * MI * NI * 4 * 64 + ln) * 4;
@@ -435,6 +486,10 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     }
     if (!has_next) break;
     cur = nxt;
+    if (asks) mail[0] = after;
+    LOSS_WAIT_LGKM0();
+    __builtin_amdgcn_s_barrier();
+    has_next = item_at(__builtin_amdgcn_readfirstlane(mail[0]), nxt);
   }
   LOSS_WAIT_VMCNT(0);
 }
@@ -624,6 +679,7 @@ __device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, 
 __global__ __launch_bounds__(256) void loss_prep_kernel(const LossPrep a) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
   __shared__ int counts[32];
+  if (blockIdx.x == 0 && threadIdx.x < kLossQueues * kGemmXcds) a.queues[threadIdx.x] = 0;
   if (int(blockIdx.x) < a.label_blocks) {
     const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (r < a.n_pad) prep_labels(a, r);
@@ -987,7 +1043,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
           float m = u[0];
 #pragma unroll
           for (int e = 1; e < 16; ++e) m = fmaxf(m, u[e]);
-          m = fmaxf(m, __shfl_xor(m, 32));
+          m = half_max(m);
           float s = 0.0f, all = 0.0f;  // as in loss_gemm_kernel
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
@@ -995,9 +1051,8 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
             s += __builtin_amdgcn_fractf(x);
             all += x;
           }
-          float ones = __builtin_rintf(all - s);
-          s += __shfl_xor(s, 32);
-          ones += __shfl_xor(ones, 32);
+          const float ones = half_sum(__builtin_rintf(all - s));
+          s = half_sum(s);
           if (fh == 0) {
             const int64_t at = int64_t(c0 >> 5) * a.ldr + row;
             a.gm[at] = m * a.inv_t;

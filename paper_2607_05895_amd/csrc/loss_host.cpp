@@ -57,7 +57,7 @@ struct Plan {
   int group = kLossGroup;       // columns of a softmax partial
   Gemm logits, dx, dw;
   // offsets
-  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, row = 0, zt = 0, gm = 0, gs = 0;
+  size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, queues = 0, row = 0, zt = 0, gm = 0, gs = 0;
   size_t xb = 0, xt = 0, wb = 0, wt = 0, codes = 0, z32 = 0, dz_t = 0, part = 0, acc = 0;
   size_t bytes = 0;
 };
@@ -65,36 +65,64 @@ struct Plan {
 // Most tokens whose products read w as it lies, and the fewest ids.
 constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
 
-// Tile and K ranges of one product of M x N with K steps: the choice whose rounds of tiles over the chip's workgroups take
-// least, a step of a 256 x 256 tile taken as 1, of two 128 x 128 tiles on one CU as 0.6, a tile's start and epilogue as 12 steps and
-// the join of the ranges as its traffic.
-Gemm choose(int64_t M, int64_t N, int64_t steps, bool may_split) {
-  Gemm best;
-  double cost = 0.0;
+// A launch's time in us on `tile` x `tile` tiles, items[i] of steps[i] K steps each: what the chip's workgroups share, or the
+// longest item if that is more, and half of the shortest kind for the uneven end. A step of 32 takes 0.74 us on a 256 x 256 tile
+// (1.45 PFLOP/s over 256 CUs) and 0.45 us on two 128 x 128 ones that share a CU (0.26 us with a CU of its own); a tile's start and epilogue about
+// as long as 12 steps.
+double launch_us(int tile, int kinds, const int64_t* items, const int64_t* steps) {
+  const bool large = tile == kLossTile;
+  double work = 0.0, longest = 0.0, shortest = 1e30;
+  int64_t count = 0;
+  for (int i = 0; i < kinds; ++i) {
+    const double len = double(steps[i]) + 12.0;
+    work += double(items[i]) * len;
+    longest = std::max(longest, len);
+    shortest = std::min(shortest, len);
+    count += items[i];
+  }
+  const double per_step = large ? 0.74 : count <= 256 ? 0.26 : 0.45;
+  const int64_t slots = std::min<int64_t>(large ? 256 : 512, count);
+  return per_step * (std::max(work / double(slots), longest) + (count > slots ? 0.5 * shortest : 0.0));
+}
+Gemm grid_of(int tile, int64_t M, int64_t N) {
+  Gemm g;
+  g.tile = tile;
+  g.tm = int(up(M, tile) / tile);
+  g.tn = int(up(N, tile) / tile);
+  return g;
+}
+// The tile of a product that runs alone.
+Gemm choose(int64_t M, int64_t N, int64_t steps) {
+  Gemm g[2] = {grid_of(kLossTile, M, N), grid_of(kLossTileSmall, M, N)};
+  double us[2];
+  for (int i = 0; i < 2; ++i) {
+    const int64_t items = g[i].items();
+    us[i] = launch_us(g[i].tile, 1, &items, &steps);
+  }
+  return g[us[1] < us[0]];
+}
+// The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K) in one launch, and the K ranges of dx: each range at least 16 steps
+// long, the join of the ranges taken as its traffic and a launch.
+void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wsteps, Gemm& dx, Gemm& dw) {
+  double best = 0.0;
+  dx.tile = 0;
   for (int tile : {kLossTile, kLossTileSmall}) {
-    const int64_t tm = up(M, tile) / tile, tn = up(N, tile) / tile, tiles = tm * tn;
-    const int64_t slots = tile == kLossTile ? 256 : 512;
-    const int most = may_split ? int(std::max<int64_t>(1, std::min<int64_t>(16, steps / 16))) : 1;
-    for (int s = 1; s <= most; ++s) {
-      const int64_t kper = (steps + s - 1) / s;
-      if ((steps + kper - 1) / kper != s) continue;
-      // 128 x 128 tiles: one workgroup per CU while there are at most 256 of them (a step then takes 0.35)
-      const int64_t items = tiles * s;
-      const double per_step = tile == kLossTile ? 1.0 : items <= 256 ? 0.35 : 0.6;
-      const double rounds = double((items + slots - 1) / slots);
-      double c = rounds * (double(kper) + 12.0) * per_step;
-      if (s > 1) c += 8.0 + double(tiles) * s * tile * tile * 8.0 / 4.9e6;
-      if (best.tile == 0 || c < cost) {
-        cost = c;
-        best.tile = tile;
-        best.tm = int(tm);
-        best.tn = int(tn);
-        best.splits = s;
-        best.kper = int(kper);
+    const Gemm x = grid_of(tile, n, h), w = grid_of(tile, v, h);
+    for (int s = 1; s <= 64 && (s == 1 || xsteps / s >= 16); ++s) {
+      const int64_t kper = (xsteps + s - 1) / s;
+      if ((xsteps + kper - 1) / kper != s) continue;
+      const int64_t items[2] = {x.items() * s, w.items()}, steps[2] = {kper, wsteps};
+      double us = launch_us(tile, 2, items, steps);
+      if (s > 1) us += 6.0 + double(items[0]) * tile * tile * 8.0 / 4.9e6;
+      if (dx.tile == 0 || us < best) {
+        best = us;
+        dx = x;
+        dw = w;
+        dx.splits = s;
+        dx.kper = int(kper);
       }
     }
   }
-  return best;
 }
 
 int check(const mfsdp_head_loss* a, int64_t k, bool pointers) {
@@ -155,15 +183,16 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
       part = size_t(p.dx.splits) * size_t(p.chunk * p.hp) * 4;
     }
   } else {
-    p.logits = choose(p.chunk, p.v, p.nseg * p.hk / 32, false);
+    p.logits = choose(p.chunk, p.v, p.nseg * p.hk / 32);
     p.logits.nk = int(p.hk / 32);
-    if (a->dx) {
-      p.dx = choose(p.chunk, p.h, p.nseg * vsteps, true);
-      p.dx.nk = int(vsteps);
-      if (p.dx.splits > 1) part = size_t(p.dx.items()) * size_t(p.dx.tile) * p.dx.tile * 4;
-    }
   }
-  if (a->dw) p.dw = choose(p.v, p.h, p.nseg * p.chunk / 32, false);
+  if (p.grads && !p.stream) {
+    choose_grads(p.chunk, p.v, p.h, p.nseg * vsteps, p.nseg * p.chunk / 32, p.dx, p.dw);
+    p.dx.nk = int(vsteps);
+    if (a->dx && p.dx.splits > 1) part = size_t(p.dx.items()) * size_t(p.dx.tile) * p.dx.tile * 4;
+  } else if (a->dw) {
+    p.dw = choose(p.v, p.h, p.nseg * p.chunk / 32);
+  }
   size_t o = 0;
   auto take = [&](int64_t bytes) {
     const size_t at = o;
@@ -177,6 +206,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.on = take(p.n_pad * 4);
   p.weighted = take(p.n_pad * 4);
   p.denom = take(4);
+  p.queues = take(kLossQueues * kGemmXcds * 4);
   p.row = take(p.chunk * 16);
   p.zt = take(p.chunk * k * 4);
   p.gm = take(groups * p.chunk * 4);
@@ -230,6 +260,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
   prep.l = LossLabels{l.ids, l.logits, l.id_bytes == 8, l.logit_dtype == MFSDP_BF16, int32_t(k), p.n, p.v, l.ignore, inv_t};
   prep.n_pad = p.n_pad;
   prep.id = reinterpret_cast<int32_t*>(ws + p.id);
+  prep.queues = reinterpret_cast<int32_t*>(ws + p.queues);
   prep.q = f32p(p.q);
   prep.ent = f32p(p.ent);
   prep.on = f32p(p.on);
@@ -314,6 +345,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       LossGemm& z = zz.g[0];
       z = product(p.logits, p.xb, p.hk, xpart, p.wb, p.hk, wpart, p.logits.nk);
       zz.count = 1;
+      zz.queue = prep.queues;
       z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
       z.rows = int(rows);
       z.cols = int(p.v);
@@ -410,9 +442,9 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (!last) mw.part = f32p(p.acc);
     }
     LossGemm2 both{};
-    // one launch where the tiles of both fit the chip at once
-    const bool together = a->dx && a->dw && !p.stream && p.dx.tile == p.dw.tile &&
-                          p.dx.items() + p.dw.items() <= (p.dx.tile == kLossTile ? 256 : 512);
+    // one launch where both use the same tile; the longer tiles first
+    const bool together = a->dx && a->dw && !p.stream && p.dx.tile == p.dw.tile;
+    both.queue = prep.queues + kGemmXcds;
     if (a->dx && p.stream) {
       LossStream s{};
       s.P = u16p(p.codes);
@@ -428,14 +460,16 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       s.ldo = p.hp;
       LOSS_TRY(launch_loss_stream(s, p.stream, kLossOut, st), "dx launch");
     } else if (a->dx) {
-      both.g[0] = mx;
-      both.g[1] = mw;
+      const bool swap = together && mw.kper > mx.kper;
+      both.g[swap ? 1 : 0] = mx;
+      both.g[swap ? 0 : 1] = mw;
       both.count = together ? 2 : 1;
       LOSS_TRY(launch_loss_gemm(both, kLossOut, p.dx.tile, st), "dx launch");
     }
     if (a->dw && !together) {
       both.g[0] = mw;
       both.count = 1;
+      both.queue = prep.queues + 2 * kGemmXcds;
       LOSS_TRY(launch_loss_gemm(both, kLossOut, p.dw.tile, st), "dw launch");
     }
     if (a->dx && (p.stream || mx.splits > 1)) {

@@ -25,6 +25,7 @@ constexpr int kLossTile = 256;       // output tile of the products (kLossTileSm
 constexpr int kLossTileSmall = 128;
 constexpr int kLossGroup = 64;       // columns of one softmax partial (of the products for a few tokens: 32)
 constexpr int kLossMaxSeg = 6;
+constexpr int kLossQueues = 3;         // launches of products per chunk that take their tiles from counters
 constexpr int kLossMaxTop = 256;     // most teacher logits a token
 constexpr float kLossOctaves = 64.0f;  // factors of two that the 16-bit codes of the logits span
 
@@ -61,6 +62,7 @@ struct LossGemm {
 struct LossGemm2 {
   LossGemm g[2];
   int32_t count;
+  int32_t* queue;  // kGemmXcds counters, 0 before the launch
 };
 
 // Products for a few tokens (at most 32 MI), where reading w counts: w is read as it lies, once, with no packed copy.
@@ -103,12 +105,13 @@ struct LossPack {
 };
 
 // The first launch: the labels in one form (per token k ids with weights q that add up to 1, -1 and 0 for none; the sum of
-// q log q; on: whether the token counts, 1, 0, or NaN for an id outside the vocabulary), and the packed operands.
+// q log q; on: whether the token counts, 1, 0, or NaN for an id outside the vocabulary), the packed operands, and the
+// counters of the chunk's products set to 0.
 struct LossPrep {
   LossLabels l;
   int64_t n_pad;
   int32_t label_blocks;        // workgroups of four tokens each; the packs' workgroups follow
-  int32_t* id;
+  int32_t *id, *queues;
   float *q, *ent, *on;
   LossPack d[2];
   int32_t packs;
