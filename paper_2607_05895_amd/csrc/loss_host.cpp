@@ -66,23 +66,25 @@ struct Plan {
 constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
 
 // A launch's time in us on `tile` x `tile` tiles, items[i] of steps[i] K steps each: what the chip's workgroups share, or the
-// longest item if that is more, and half of the shortest kind for the uneven end. A step of 32 takes 0.74 us on a 256 x 256 tile
-// (1.45 PFLOP/s over 256 CUs) and 0.45 us on two 128 x 128 ones that share a CU (0.26 us with a CU of its own); a tile's start and epilogue about
-// as long as 12 steps.
+// longest item if that is more, and half of the shortest kind for the uneven end. Measured: a step of 32 takes 0.74 us on a
+// 256 x 256 tile (1.45 PFLOP/s over 256 CUs) and a tile's start and epilogue 8 us; on 128 x 128 tiles 0.3 and 5 us with a CU of their
+// own, 0.55 and 13 us on two that share one (4096 tokens, 20000 x 4096 head, dx and dw: 1064 us on 256 x 256 tiles, 1433 on
+// 128 x 128; 200 tokens, 2000 x 2048: 30 and 23 us).
 double launch_us(int tile, int kinds, const int64_t* items, const int64_t* steps) {
-  const bool large = tile == kLossTile;
-  double work = 0.0, longest = 0.0, shortest = 1e30;
   int64_t count = 0;
-  for (int i = 0; i < kinds; ++i) {
-    const double len = double(steps[i]) + 12.0;
-    work += double(items[i]) * len;
-    longest = std::max(longest, len);
-    shortest = std::min(shortest, len);
-    count += items[i];
-  }
-  const double per_step = large ? 0.74 : count <= 256 ? 0.26 : 0.45;
+  for (int i = 0; i < kinds; ++i) count += items[i];
+  const bool large = tile == kLossTile, alone = count <= 256;
+  const double per_step = large ? 0.74 : alone ? 0.3 : 0.55, ends = large ? 8.0 : alone ? 5.0 : 13.0;
   const int64_t slots = std::min<int64_t>(large ? 256 : 512, count);
-  return per_step * (std::max(work / double(slots), longest) + (count > slots ? 0.5 * shortest : 0.0));
+  double work = 0.0, longest = 0.0, shortest = 1e30;
+  for (int i = 0; i < kinds; ++i) {
+    if (items[i] == 0) continue;
+    const double us = per_step * double(steps[i]) + ends;
+    work += double(items[i]) * us;
+    longest = std::max(longest, us);
+    shortest = std::min(shortest, us);
+  }
+  return std::max(work / double(std::max<int64_t>(slots, 1)), longest) + (count > slots ? 0.5 * shortest : 0.0);
 }
 Gemm grid_of(int tile, int64_t M, int64_t N) {
   Gemm g;
@@ -101,8 +103,8 @@ Gemm choose(int64_t M, int64_t N, int64_t steps) {
   }
   return g[us[1] < us[0]];
 }
-// The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K) in one launch, and the K ranges of dx: each range at least 16 steps
-// long, the join of the ranges taken as its traffic and a launch.
+// The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K; 0: not asked for) in one launch, and the K ranges of dx: each range
+// at least 16 steps long, the join of the ranges taken as its traffic and a launch.
 void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wsteps, Gemm& dx, Gemm& dw) {
   double best = 0.0;
   dx.tile = 0;
@@ -111,7 +113,7 @@ void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wstep
     for (int s = 1; s <= 64 && (s == 1 || xsteps / s >= 16); ++s) {
       const int64_t kper = (xsteps + s - 1) / s;
       if ((xsteps + kper - 1) / kper != s) continue;
-      const int64_t items[2] = {x.items() * s, w.items()}, steps[2] = {kper, wsteps};
+      const int64_t items[2] = {x.items() * s, wsteps ? w.items() : 0}, steps[2] = {kper, wsteps};
       double us = launch_us(tile, 2, items, steps);
       if (s > 1) us += 6.0 + double(items[0]) * tile * tile * 8.0 / 4.9e6;
       if (dx.tile == 0 || us < best) {
@@ -183,15 +185,20 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
       part = size_t(p.dx.splits) * size_t(p.chunk * p.hp) * 4;
     }
   } else {
-    p.logits = choose(p.chunk, p.v, p.nseg * p.hk / 32);
+    p.logits = choose(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.nseg * p.hk / 32);
     p.logits.nk = int(p.hk / 32);
   }
-  if (p.grads && !p.stream) {
-    choose_grads(p.chunk, p.v, p.h, p.nseg * vsteps, p.nseg * p.chunk / 32, p.dx, p.dw);
+  const int64_t wsteps = p.nseg * up(std::min(p.chunk, std::max<int64_t>(p.n, 1)), 32) / 32;
+  if (a->dx && !p.stream) {
+    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.nseg * vsteps, a->dw ? wsteps : 0, p.dx, p.dw);
     p.dx.nk = int(vsteps);
-    if (a->dx && p.dx.splits > 1) part = size_t(p.dx.items()) * size_t(p.dx.tile) * p.dx.tile * 4;
+    // room for the ranges of dx alone too: a call with fewer outputs never needs more workspace
+    Gemm alone, none;
+    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.nseg * vsteps, 0, alone, none);
+    for (const Gemm& g : {p.dx, alone})
+      if (g.splits > 1) part = std::max(part, size_t(g.items()) * size_t(g.tile) * g.tile * 4);
   } else if (a->dw) {
-    p.dw = choose(p.v, p.h, p.nseg * p.chunk / 32);
+    p.dw = choose(p.v, p.h, wsteps);
   }
   size_t o = 0;
   auto take = [&](int64_t bytes) {
@@ -221,7 +228,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   }
   if (a->dw) p.dz_t = take(p.vp * p.chunk * es);
   p.part = take(int64_t(part));
-  if (a->dw && p.chunk < p.n) p.acc = take(p.dw.items() * p.dw.tile * p.dw.tile * 4);
+  if (a->dw && p.chunk < p.n) p.acc = take(p.vp * p.hp * 4);
   p.bytes = o;
   return p;
 }

@@ -91,6 +91,15 @@ def test_workspace_does_not_hold_the_logits():
         assert size(n=n) < 4 * (1 << 30)
 
 
+@pytest.mark.parametrize("dtype", [native.BF16, native.F32])
+@pytest.mark.parametrize("n,v,h", [(1, 1, 1), (48, 128256, 4096), (200, 5000, 130), (1024, 20000, 4096), (70000, 3000, 64)])
+def test_fewer_outputs_never_need_more_workspace(n, v, h, dtype):
+    size = lambda **kw: native.mfsdp_head_loss_workspace_size(_args(n=n, v=v, h=h, dtype=dtype, **kw))  # noqa: E731
+    both = size()
+    for fewer in (dict(dx=None), dict(dw=None), dict(dx=None, dw=None)):
+        assert size(**fewer) <= both
+
+
 def test_cpu_tensors_are_refused():
     x, w, t = torch.zeros(4, 8), torch.zeros(16, 8), torch.zeros(4, dtype=torch.int64)
     with pytest.raises(ValueError, match="CUDA"):
