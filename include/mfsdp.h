@@ -474,6 +474,10 @@ int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t i
                          int32_t logit_dtype, int32_t k, double temperature, void* workspace, size_t workspace_bytes,
                          void* stream);
 
+/* grad <- factor[0] grad in place (device fp32 factor; numel elements of dtype F32 or BF16, rounded to nearest even): a
+ * gradient of loss as the gradient of what loss went into. A factor of exactly 1 leaves it as it is, at the cost of a launch. */
+int mfsdp_scale_grad(void* grad, int64_t numel, int32_t dtype, const float* factor, void* stream);
+
 /* ---- Owner planning (host only; no GPU, no stream) ---------------------------------------- */
 
 /* Planner policies (Algorithm 1, "Balance-aware owner planning"). */

@@ -1109,6 +1109,34 @@ __global__ __launch_bounds__(256) void loss_zero_kernel(uint16_t* p, int64_t n) 
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) p[i] = 0;
 }
 
+// Eight elements per thread and pass; p is 16-byte aligned.
+__global__ __launch_bounds__(256) void scale_grad_kernel(void* p, int64_t n, int bf16, const float* factor) {
+  const float f = *factor;
+  if (f == 1.0f) return;
+  for (int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8; i < n; i += int64_t(gridDim.x) * 256 * 8) {
+    if (bf16) {
+      uint16_t* q = (uint16_t*)p + i;
+      if (i + 8 <= n) {
+        u32x4 v = *(gptr<u32x4>)q;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          v[t] = pack_bf16x2(__uint_as_float(v[t] << 16) * f, __uint_as_float(v[t] & 0xffff0000u) * f);
+        *(gptr<u32x4>)q = v;
+      } else {
+        for (int t = 0; i + t < n; ++t) q[t] = uint16_t(pack_bf16x2(__uint_as_float(uint32_t(q[t]) << 16) * f, 0.0f));
+      }
+    } else {
+      float* q = (float*)p + i;
+      if (i + 8 <= n) {
+        *(gptr<f32x4_t>)q = *(gptr<f32x4_t>)q * f;
+        *(gptr<f32x4_t>)(q + 4) = *(gptr<f32x4_t>)(q + 4) * f;
+      } else {
+        for (int t = 0; i + t < n; ++t) q[t] *= f;
+      }
+    }
+  }
+}
+
 template <int NW, int TB, int KIND>
 void launch_gemm_seg(const LossGemm2& a, hipStream_t st) {
   const dim3 grid(kGemmXcds * Grid<NW, TB>::SLOTS), block(NW * 64);
@@ -1192,6 +1220,14 @@ hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st) {
   if (n > 0) {
     const int64_t g = (n + 255) / 256;
     hipLaunchKernelGGL(loss_zero_kernel, dim3(unsigned(g < 4096 ? g : 4096)), dim3(256), 0, st, (uint16_t*)p, n);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_scale_grad(void* p, int64_t n, int bf16, const float* factor, hipStream_t st) {
+  if (n > 0) {
+    const int64_t g = (n + 2047) / 2048;
+    hipLaunchKernelGGL(scale_grad_kernel, dim3(unsigned(g < 8192 ? g : 8192)), dim3(256), 0, st, p, n, bf16, factor);
   }
   return hipGetLastError();
 }

@@ -533,4 +533,13 @@ int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t i
   return run(args, k, Labels{ids, logits, id_bytes, logit_dtype, 0, temperature, 0.0}, workspace, workspace_bytes, stream);
 }
 
+int mfsdp_scale_grad(void* grad, int64_t numel, int32_t dtype, const float* factor, void* stream) {
+  if (numel < 0) return fail(MFSDP_E_INVALID, "numel must be >= 0");
+  if (dtype != MFSDP_F32 && dtype != MFSDP_BF16) return fail(MFSDP_E_INVALID, "unsupported dtype");
+  if (!factor || (numel > 0 && !grad)) return fail(MFSDP_E_INVALID, "NULL pointer");
+  if (!aligned16(grad)) return fail(MFSDP_E_INVALID, "pointers must be 16-byte aligned");
+  const hipError_t e = launch_scale_grad(grad, numel, dtype == MFSDP_BF16, factor, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? MFSDP_OK : hip_fail(e, "scale launch");
+}
+
 }  // extern "C"

@@ -183,6 +183,7 @@ hipError_t launch_loss_total(const LossTotal& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st);
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st);
 hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st);
+hipError_t launch_scale_grad(void* p, int64_t n, int bf16, const float* factor, hipStream_t st);
 // Rows of one workgroup of the rows launch.
 constexpr int loss_rows_per_block(int rows_pad) { return rows_pad <= 256 ? 4 : 32; }
 

@@ -25,7 +25,7 @@ EXPORTS = ("mfsdp_muon_workspace_size", "mfsdp_muon_step", "mfsdp_muon_step_time
            "mfsdp_inverse_root", "mfsdp_soap_workspace_size", "mfsdp_soap_step",
            "mfsdp_orthonormal_factor_workspace_size", "mfsdp_orthonormal_factor", "mfsdp_build_id",
            "mfsdp_muon_step_noalloc", "mfsdp_plan_layouts", "mfsdp_head_loss_workspace_size", "mfsdp_linear_xent",
-           "mfsdp_linear_distill")
+           "mfsdp_linear_distill", "mfsdp_scale_grad")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 MAX_GRAD_PARTS = 64
 ABI_VERSION = 6
@@ -183,6 +183,8 @@ def lib() -> ctypes.CDLL:
         L.mfsdp_linear_xent.restype = ctypes.c_int
         L.mfsdp_linear_distill.argtypes = [ctypes.POINTER(HeadLoss), vp, i32, vp, i32, i32, f64, vp, sz, vp]
         L.mfsdp_linear_distill.restype = ctypes.c_int
+        L.mfsdp_scale_grad.argtypes = [vp, i64, i32, vp, vp]
+        L.mfsdp_scale_grad.restype = ctypes.c_int
         L.mfsdp_build_id.argtypes = []
         L.mfsdp_build_id.restype = ctypes.c_char_p
         from . import build_lib
@@ -383,6 +385,10 @@ def mfsdp_linear_distill(args: HeadLoss, ids: int, id_bytes: int, logits: int, l
                          temperature: float, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
     _check(lib().mfsdp_linear_distill(ctypes.byref(args), ids, id_bytes, logits, logit_dtype, k, temperature,
                                       workspace, workspace_bytes, stream))
+
+
+def mfsdp_scale_grad(grad: int, numel: int, dtype: int, factor: int, stream: int = 0) -> None:
+    _check(lib().mfsdp_scale_grad(grad, numel, dtype, factor, stream))
 
 
 # ------------------------------------------------------------------- torch tensor helpers
@@ -641,3 +647,10 @@ def linear_distill_t(x, w, ids, logits, loss=None, token_loss=None, lse=None, dx
     if workspace is None:
         workspace = head_loss_workspace_t(args, k, x.device)
     mfsdp_linear_distill(args, ip, ids.element_size(), lp, _dt(logits), k, float(temperature), *_ws(workspace), _stream())
+
+
+def scale_grad_t(grad, factor) -> None:
+    """grad <- factor grad in place; factor: a float32 tensor of one element on the same GPU."""
+    if factor.numel() != 1:
+        raise ValueError(f"factor: one element is required, got shape {tuple(factor.shape)}")
+    mfsdp_scale_grad(_ptr(grad, "grad"), grad.numel(), _dt(grad), _ptr(factor, "factor", None, ("float32",)), _stream())

@@ -108,6 +108,23 @@ def test_cpu_tensors_are_refused():
         native.linear_distill_t(x, w, t[:, None], torch.zeros(4, 1), loss=torch.zeros(1))
 
 
+def test_front_ends_refuse_cpu_tensors():
+    from paper_2607_05895_amd import losses
+    x, w, t = torch.zeros(2, 4, 8), torch.zeros(16, 8), torch.zeros(2, 4, dtype=torch.int64)
+    for call in (lambda: losses.linear_cross_entropy(x, w, t), lambda: losses.token_losses(x, w, t),
+                 lambda: losses.linear_distillation(x, w, t[..., None], torch.zeros(2, 4, 1))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
+@pytest.mark.parametrize("grad,numel,dt,factor", [(FAKE, -1, 0, FAKE), (FAKE, 4, 2, FAKE), (None, 4, 0, FAKE),
+                                                  (FAKE, 4, 0, None), (FAKE + 4, 4, 0, FAKE)])
+def test_bad_scale_arguments_are_refused(grad, numel, dt, factor):
+    with pytest.raises(native.MfsdpError) as ei:
+        native.mfsdp_scale_grad(grad, numel, dt, factor)
+    assert ei.value.status == native.E_INVALID
+
+
 def test_struct_matches_the_header():
     """8-byte fields and pairs of 4-byte ones: no padding anywhere."""
     assert ctypes.sizeof(native.HeadLoss) == 8 * 14
