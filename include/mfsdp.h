@@ -446,8 +446,9 @@ typedef struct {
   int64_t chunk_rows;
 } mfsdp_head_loss;
 
-/* Bytes of device workspace for mfsdp_linear_xent (k = 1) and mfsdp_linear_distill with these arguments: copies of w (and
- * of w^T for dx), the chunk's logits and their transpose, and for n beyond one chunk an fp32 sum of dw. Of the pointers
+/* Bytes of device workspace for mfsdp_linear_xent (k = 1) and mfsdp_linear_distill with these arguments: the chunk's rows of
+ * x and (for gradients) its logits, a copy of w for F32 (three bf16 parts) and for h that are no multiple of 8, and for n
+ * beyond one chunk an fp32 sum of dw. Of the pointers
  * only whether dx and dw are NULL is looked at. 0 on invalid arguments. */
 size_t mfsdp_head_loss_workspace_size(const mfsdp_head_loss* args, int32_t k);
 

@@ -46,13 +46,24 @@ __device__ __forceinline__ int swz(int r) { return ((r >> 1 ^ r >> 3) & 1) | (((
 #define LOSS_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | (((n) >> 4) << 14) | (7 << 4) | (0xF << 8))
 #define LOSS_WAIT_LGKM0() __builtin_amdgcn_s_waitcnt(0xF | (7 << 4) | (0 << 8) | (3 << 14))
 
+// A transposing read (four rows by one column per lane and 16 lanes). Through a restrict pointer: without alias information of
+// their own the compiler takes these reads to depend on every load into LDS in flight and waits for all of them
+// (8192 x 4096 x 128256: 0.99 PFLOP/s so, 1.47 without those waits, as with plain reads of a transposed copy).
+__device__ __forceinline__ bf16x4_t read_tr(lptr<bf16x4_t> __restrict p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(p);
+}
+__device__ __forceinline__ bf16x8_t join_tr(bf16x4_t lo, bf16x4_t hi) {
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // NW waves, 2 x NW/2, on a TB x TB tile; a wave's part is MI x 2 blocks of 32 x 32.
 template <int NW, int TB>
 struct Grid {
   static constexpr int WN = NW / 2;
   static constexpr int MI = TB / 64, NI = 2;
   static_assert(WN * 64 == TB, "64 columns a wave");
-  static constexpr int STAGE = 2 * TB * kRowB;
+  static constexpr int HALF = TB * kRowB;                 // bytes of one operand's step of 32
+  static constexpr int STAGE = 2 * HALF;
   static constexpr int DW = NW == 8 ? 4 : NW;             // waves that issue the loads
   static constexpr int PL = TB / kBlkRows / DW;           // loads of P (and of Q) per issuing wave and step
   static constexpr int DLOADS = 2 * PL;
@@ -86,15 +97,25 @@ struct Item {
   int p, bi, bj, k0, nk;  // problem, tile, K steps
 };
 
-// C = P Q^T on a persistent grid. The main loop is the one of the Newton-Schulz products: a five-stage LDS ring filled by
-// direct global->LDS loads of whole 1 KiB blocks by one wave of each SIMD, one barrier per K step of 32 inside its second
-// 16-wide slice, the next step's fragments read while the rest of that slice multiplies, and the next tile's first loads
-// issued before this tile's epilogue. Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
+// Tiles of P Q^T on a persistent grid, all operands as they lie:
+//   logits  P = x (panel blocked),  Q = w, rows of K;             K = h
+//   dx      P = dz (panel blocked), Q = w, read transposed;       K = v
+//   dw      P = dz, Q = x (panel blocked), both read transposed;  K = tokens
+// LDS is filled by direct loads, from one wave of each SIMD, of whole 1 KiB blocks of a panel-blocked operand (16 rows by 32
+// columns) or of whole 128-byte lines of w. One barrier per K step of 32 inside its second 16-wide slice; the next step's
+// fragments are read while the rest of that slice multiplies, and the next tile's first loads are issued before this
+// tile's epilogue. dx, dw: a ring of five steps, filled four steps ahead. logits: w's lines span two steps, so w has a ring
+// of three pairs of steps and x one of four steps (three ahead).
+// The order in the loops is the instruction order: left to itself the compiler gathers the loads (which write LDS) between
+// the LDS reads, and the MFMAs wait behind them (8192 x 4096 x 128256: 1.19 PFLOP/s so, 1.50 in this order).
+// Tiles are dealt to the XCDs in groups that share operand panels in L2 (bands of BAND block rows, column by
 // column) and taken from counters, so that long and short tiles (the K ranges of dx, the tiles of dw) share the chip evenly.
 template <int NW, int TB, int NSEG, int KIND>
 __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm2 b) {
   using G = Grid<NW, TB>;
-  constexpr int MI = G::MI, NI = G::NI, STAGE = G::STAGE, DW = G::DW, PL = G::PL, DLOADS = G::DLOADS;
+  constexpr int MI = G::MI, NI = G::NI, HALF = G::HALF, STAGE = G::STAGE, DW = G::DW, PL = G::PL, DLOADS = G::DLOADS;
+  constexpr int kSlabAt = (kStages - 1) * STAGE;  // the part of LDS that no tile's first loads touch
+  constexpr int kQAt = 4 * HALF;                  // logits: w's pairs of steps behind x's four steps
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * STAGE];
 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -151,62 +172,162 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   };
 
   const bool issuer = w < DW;
-  // load i of P (of Q) of issuing wave w moves the 1 KiB block of 16-row panel i DW + w: lane l its row l / 4, 16-byte chunk
-  // (l % 4) ^ swz(row), so that the fragment reads are conflict-free. One lane offset for all; the rest is scalar.
+  // Lane offsets (bytes) of a load: a 1 KiB block (lane l: row l / 4, 16-byte chunk (l % 4) ^ swz(row), so that the plain fragment
+  // reads are conflict-free); eight 128-byte lines of w (row l / 8, chunk (l % 8) ^ (row / 2) % 8); 64 lanes along TB columns of
+  // w's rows (chunk ^ 4 (row % 4)). Loads past w's last 16 bytes are held there: what they bring meets zeros of x or dz, or
+  // belongs to columns that are not stored.
   const uint32_t loff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
-  uint32_t pstep = 0, qstep = 0;
-  int lp = 0;  // its problem
-  const uint16_t *pbase_g = nullptr, *qbase_g = nullptr;  // the wave's first panels of the tile being loaded
-  __amdgpu_buffer_rsrc_t pr, qr;
-  auto rsrc = [](const uint16_t* p) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00020000); };
+  constexpr int RPL = 512 / TB;  // rows of w per load of TB columns
+  // of the tile whose loads are being issued
+  uint32_t qlane = 0, prow32 = 0, qrow2 = 0, qrow32 = 0;
+  const char *pbase = nullptr, *qbase = nullptr;
+  int64_t wleft = 0, ppart = 0, qpart = 0, pstep = 0, qstep = 0;  // bytes: of w from qbase; between parts; of one step
+  int seg_steps = 1;
+  bool dw = false;
   auto aim = [&](const Item& it) {
     const LossGemm& a = b.g[it.p];
-    lp = it.p;
-    pstep = DW * kBlkRows * 2 * uint32_t(a.ldp);
-    qstep = DW * kBlkRows * 2 * uint32_t(a.ldq);
-    pbase_g = a.P + (int64_t(it.bi) * TB + w * kBlkRows) * a.ldp;
-    qbase_g = a.Q + (int64_t(it.bj) * TB + w * kBlkRows) * a.ldq;
-    if constexpr (NSEG == 1) {
-      pr = rsrc(pbase_g);
-      qr = rsrc(qbase_g);
+    dw = KIND == kLossOut && a.op == kLossDw;
+    prow32 = uint32_t(a.ldp * 32);   // a 16-row panel
+    qrow2 = uint32_t(a.ldq * 2);
+    qrow32 = uint32_t(a.ldq * 32);
+    ppart = a.ppart * 2;
+    qpart = a.qpart * 2;
+    seg_steps = a.nk;
+    if (dw) {
+      pbase = (const char*)(a.P + int64_t(it.bi) * (TB * kBlkRows));
+      qbase = (const char*)(a.Q + int64_t(it.bj) * (TB * kBlkRows));
+      pstep = a.ldp * 64;
+      qstep = a.ldq * 64;
+    } else {
+      pbase = (const char*)(a.P + (int64_t(it.bi) * TB + w * kBlkRows) * a.ldp);
+      pstep = 1024;
+      const int64_t row = a.ldq * 2, at = KIND == kLossLogits ? int64_t(it.bj) * TB * row : int64_t(it.bj) * TB * 2;
+      qbase = (const char*)a.Q + at;
+      qstep = row * 32;
+      wleft = a.qrows * row - at;
+      if constexpr (KIND == kLossLogits)
+        qlane = uint32_t((w * 8 + (lane >> 3)) * row) + ((lane & 7) ^ (((w & 1) * 4 + (lane >> 4)) & 7)) * 16;
+      else
+        qlane = uint32_t((w * RPL + lane / (TB / 8)) * row) +
+                ((lane % (TB / 8)) ^ (((w * RPL + lane / (TB / 8)) & 3) << 2)) * 16;
     }
   };
-  // load l (0 .. PL - 1: of P, then of Q) of step k of all segments
-  auto issue = [&](int l, int k, int stage) {
-    int kk = k;
+  auto load = [&](const char* base, uint32_t voff, uint32_t soff, int at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00020000),
+                                             (lds_byte*)(smem + at), 16, voff, soff, 0, 0);
+  };
+  // Step k of all segments: the step in its segment, and the bytes to its parts of P and Q. fp32 operands lie in three bf16
+  // parts; the pairs (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0), the small products first: they are added while the sum is small.
+  auto in_segment = [&](int k, int64_t& po, int64_t& qo) {
+    po = qo = 0;
     if constexpr (NSEG > 1) {
-      const LossGemm& a = b.g[lp];
-      const int sg = k / a.nk;
-      kk = k - sg * a.nk;
-      if (l < PL) pr = rsrc(pbase_g + a.pseg[sg]);
-      else qr = rsrc(qbase_g + a.qseg[sg]);
+      const int sg = k / seg_steps;
+      po = int64_t(0x001102 >> (4 * sg) & 0xf) * ppart;
+      qo = int64_t(0x010120 >> (4 * sg) & 0xf) * qpart;
+      k -= sg * seg_steps;
     }
-    const int i = l < PL ? l : l - PL;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        l < PL ? pr : qr, (lds_byte*)(smem + stage * STAGE + (l < PL ? 0 : TB * kRowB) + (i * DW + w) * 1024), 16, loff,
-        uint32_t(i) * (l < PL ? pstep : qstep) + uint32_t(kk) * 1024u, 0, 0);
+    return k;
   };
-  // the first steps of a tile (past its end: its last step again, into stages nobody reads)
+  // load i (of PL) of step k of P, of Q, into `at`. A blocked operand's next step is one block further along each panel, or (read
+  // transposed) two panels further down; load i moves block i DW + w of the step.
+  auto issue_blocked = [&](const char* base, uint32_t row32, int i, int at, auto trans_c) {
+    const int blk = i * DW + w;
+    if constexpr (decltype(trans_c)::value)
+      load(base, loff, uint32_t(blk / (TB / 32)) * row32 + (blk % (TB / 32)) * 1024, at + blk * 1024);
+    else
+      load(base, loff, uint32_t(i * DW) * row32, at + blk * 1024);
+  };
+  auto issue_p = [&](int i, int k, int at, auto trans_c) {
+    int64_t po, qo;
+    const int kk = in_segment(k, po, qo);
+    issue_blocked(pbase + po + kk * pstep, prow32, i, at, trans_c);
+  };
+  auto issue_q = [&](int i, int k, int at, auto trans_c) {  // dx, dw
+    int64_t po, qo;
+    const int kk = in_segment(k, po, qo);
+    const int64_t off = kk * qstep;
+    if constexpr (decltype(trans_c)::value) {
+      issue_blocked(qbase + qo + off, qrow32, i, at, trans_c);
+    } else {  // rows (i DW + w) RPL .. of the 32
+      const int64_t left = wleft - off;
+      const uint32_t most = uint32_t(left < 0x7ffffff0 ? left : 0x7ffffff0) - 16, v = qlane + uint32_t(i * DW * RPL) * qrow2;
+      load(qbase + qo + off, v < most ? v : most, 0, at + (i * DW + w) * 1024);
+    }
+  };
+  auto issue_w = [&](int i, int u, int at) {  // logits: load i (of 2 PL) of pair u of steps
+    int64_t po, qo;
+    const int kk = in_segment(u * 2, po, qo);
+    const uint32_t most = uint32_t(wleft < 0x7ffffff0 ? wleft : 0x7ffffff0) - 16;
+    const uint32_t v = qlane + uint32_t(i * DW * 8) * qrow2 + uint32_t(kk) * 64;
+    load(qbase + qo, v < most ? v : most, 0, at + (i * DW + w) * 1024);
+  };
+  // the first steps of a tile (past its end: its last step again, into places nobody reads)
   auto prologue = [&](const Item& it) {
     aim(it);
+    if constexpr (KIND == kLossLogits) {
+      const int units = it.nk / 2;
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s)
+      for (int i = 0; i < 2 * PL; ++i) issue_w(i, 0, kQAt);
 #pragma unroll
-      for (int l = 0; l < DLOADS; ++l) issue(l, it.k0 + min(s, it.nk - 1), s);
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < PL; ++i) issue_p(i, s, s * HALF, std::false_type{});
+#pragma unroll
+      for (int i = 0; i < 2 * PL; ++i) issue_w(i, min(1, units - 1), kQAt + 2 * HALF);
+#pragma unroll
+      for (int i = 0; i < PL; ++i) issue_p(i, min(2, it.nk - 1), 2 * HALF, std::false_type{});
+    } else {
+      auto steps = [&](auto trans_c) {
+#pragma unroll
+        for (int s = 0; s < kStages - 1; ++s) {
+          const int k = it.k0 + min(s, it.nk - 1);
+#pragma unroll
+          for (int i = 0; i < PL; ++i) issue_p(i, k, s * STAGE, trans_c);
+#pragma unroll
+          for (int i = 0; i < PL; ++i) issue_q(i, k, s * STAGE + HALF, trans_c);
+        }
+      };
+      if (dw) steps(std::true_type{});
+      else steps(std::false_type{});
+    }
   };
 
+  // Fragment addresses: plain (row lane % 32 of a block of 32, chunk 2 slice + lane / 32) and transposed (lane: rows lane / 4 % 4
+  // (+ 4) + 8 (lane / 32), columns 4 (lane % 4) + 16 (lane / 16 % 2) of 32).
   const int frow = lane & 31, fhalf = lane >> 5;
-  const int pbase = (wm * (MI * 32) + frow) * kRowB;
-  const int qbase = (TB + wn * (NI * 32) + frow) * kRowB;
-  const int slot0 = ((0 + fhalf) ^ swz(frow)) * 16;
-  const int slot1 = ((2 + fhalf) ^ swz(frow)) * 16;
-  constexpr int NMF = MI * NI, NRD = MI + NI;  // MFMAs and fragment reads per 16-wide slice
+  const int prow = (wm * (MI * 32) + frow) * kRowB, slot0 = ((0 + fhalf) ^ swz(frow)) * 16, slot1 = ((2 + fhalf) ^ swz(frow)) * 16;
+  const int trow = (lane >> 5) * 8 + ((lane >> 2) & 3), tchunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1), tbyte = (lane & 1) * 8;
+  const int tlo = trow * kRowB + ((tchunk ^ swz(trow)) << 4) + tbyte;            // in a 1 KiB block
+  const int thi = (trow + 4) * kRowB + ((tchunk ^ swz(trow + 4)) << 4) + tbyte;
+  auto frag_blocked = [&](int at, int block) {
+    lds_byte* q = (lds_byte*)(smem + at) + block * 1024;
+    return join_tr(read_tr((lptr<bf16x4_t>)(q + tlo)), read_tr((lptr<bf16x4_t>)(q + thi)));
+  };
+  auto frag_p = [&](int at, int i, int sl, auto trans_c) -> bf16x8_t {
+    if constexpr (decltype(trans_c)::value) return frag_blocked(at, sl * (TB / 32) + wm * MI + i);
+    else return *reinterpret_cast<const bf16x8_t*>(smem + at + prow + (sl ? slot1 : slot0) + i * 32 * kRowB);
+  };
+  auto frag_q = [&](int at, int j, int sl, auto trans_c) -> bf16x8_t {  // dx, dw
+    if constexpr (decltype(trans_c)::value) {
+      return frag_blocked(at, sl * (TB / 32) + wn * NI + j);
+    } else {  // w's rows of TB columns
+      const int s16 = (wn * NI + j) * 4 + tchunk;
+      lds_byte* q = (lds_byte*)(smem + at) + (sl * 16 + trow) * (TB * 2) + ((s16 ^ ((trow & 3) << 2)) << 4) + tbyte;
+      return join_tr(read_tr((lptr<bf16x4_t>)q), read_tr((lptr<bf16x4_t>)(q + 4 * (TB * 2))));
+    }
+  };
+  const int wrow = (wn * (NI * 32) + frow) * 128, wswz = (frow >> 1) & 7;
+  auto frag_w = [&](int at, int j, int sl) {  // slice sl (of 4) of a pair of steps
+    return *reinterpret_cast<const bf16x8_t*>(smem + at + wrow + (((sl * 2 + fhalf) ^ wswz) << 4) + j * 32 * 128);
+  };
+  constexpr int NMF = MI * NI, NRD = MI + NI;  // MFMAs and fragments per 16-wide slice
+  static_assert(DLOADS == NMF && PL == NMF / 2, "half of the loads in each half");
 
   Item cur, nxt;
   if (!item_at(home * per + place, cur)) return;
   if (issuer) prologue(cur);
-  // (the last stage is free whenever items are taken; the last wave asks: of eight waves it issues no loads to wait behind)
-  int* mail = reinterpret_cast<int*>(smem + (kStages - 1) * STAGE);
+  // (the last part of LDS is free whenever items are taken; the last wave asks: of eight waves it issues no loads to wait behind)
+  int* mail = reinterpret_cast<int*>(smem + kSlabAt);
   const bool asks = threadIdx.x == (NW - 1) * 64, queued = groups > kGemmXcds;
   bool has_next = false;
   if (queued) {
@@ -216,7 +337,6 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     has_next = item_at(__builtin_amdgcn_readfirstlane(mail[0]), nxt);
   }
   while (true) {
-
     f32x16_t acc[MI][NI];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -226,73 +346,121 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
     bf16x8_t pf[2][MI], qf[2][NI];  // fragments of the two slices
-    auto read_frag = [&](int r, int stage, int sl) {
-      const uint8_t* sb = smem + stage * STAGE + (sl ? slot1 : slot0);
-      if (r < MI) pf[sl][r] = *reinterpret_cast<const bf16x8_t*>(sb + pbase + r * 32 * kRowB);
-      else qf[sl][r - MI] = *reinterpret_cast<const bf16x8_t*>(sb + qbase + (r - MI) * 32 * kRowB);
-    };
     auto mfma = [&](int m, int sl) {
       const int i = m / NI, j = (i & 1) ? NI - 1 - m % NI : m % NI;
       acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[sl][j], pf[sl][i], acc[i][j], 0, 0, 0);
     };
-    // The order below is the instruction order: left to itself the compiler gathers the loads (which write LDS) between
-    // the LDS reads, and the MFMAs wait behind them. 8192 x 4096 x 128256: 1.19 PFLOP/s so, 1.45 in this order.
-    auto main_loop = [&](auto issue_c) {
-      constexpr bool ISS = decltype(issue_c)::value;
-      const int nk = cur.nk, last = cur.k0 + nk - 1;
-      if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 2) * DLOADS);
+    // One step: the first slice with the second one's reads and P's loads; half of the second slice with Q's loads; the
+    // barrier; the rest with the next step's first reads. wait_c: loads that may still be in flight for the next step to have landed.
+    auto step = [&](auto iss_c, auto wait_c, auto read1, auto read0, auto load_p, auto load_q) {
+      constexpr bool ISS = decltype(iss_c)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<NMF>([&](auto tc) {
+        constexpr int t = decltype(tc)::value;
+        mfma(t, 0);
+        if constexpr (t < NRD) read1(t);
+        if constexpr (ISS && t % 2 == 1) load_p(t / 2);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      static_for<NMF / 2>([&](auto tc) {
+        constexpr int t = decltype(tc)::value;
+        mfma(t, 1);
+        if constexpr (ISS) load_q(t);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (ISS) LOSS_WAIT_VMCNT(decltype(wait_c)::value);
       __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<NMF / 2>([&](auto tc) {
+        constexpr int t = decltype(tc)::value, R0 = t * NRD / (NMF / 2), R1 = (t + 1) * NRD / (NMF / 2);
+        mfma(NMF / 2 + t, 1);
 #pragma unroll
-      for (int r = 0; r < NRD; ++r) read_frag(r, 0, 0);
-      int cs = 0, ns = 1, fs = kStages - 1;  // stages of steps kt, kt + 1, kt + kStages - 1
-      for (int kt = 0; kt < nk; ++kt) {
-        const int kl = min(cur.k0 + kt + kStages - 1, last);
+        for (int r = R0; r < R1; ++r) read0(r);
         __builtin_amdgcn_sched_barrier(0);
-        // first slice, with the second one's reads and half of the loads
-        static_for<NMF>([&](auto tc) {
-          constexpr int t = decltype(tc)::value;
-          mfma(t, 0);
-          if constexpr (t < NRD) read_frag(t, cs, 1);
-          if constexpr (ISS && t % 2 == 1) issue(t / 2, kl, fs);
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        static_assert(DLOADS == NMF, "half of the loads in each half");
-        static_for<NMF / 2>([&](auto tc) {
-          constexpr int t = decltype(tc)::value;
-          mfma(t, 1);
-          if constexpr (ISS) issue(NMF / 2 + t, kl, fs);
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        if constexpr (ISS) LOSS_WAIT_VMCNT((kStages - 2) * DLOADS);  // step kt + 1 has landed
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        // the rest of the second slice, with the next step's first reads
-        static_for<NMF / 2>([&](auto tc) {
-          constexpr int t = decltype(tc)::value, R0 = t * NRD / (NMF / 2), R1 = (t + 1) * NRD / (NMF / 2);
-          mfma(NMF / 2 + t, 1);
-#pragma unroll
-          for (int r = R0; r < R1; ++r) read_frag(r, ns, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        cs = ns;
-        ns = (ns + 1 == kStages) ? 0 : ns + 1;
-        fs = (fs + 1 == kStages) ? 0 : fs + 1;
-      }
+      });
     };
-    if (issuer)
-      main_loop(std::true_type{});
-    else
-      main_loop(std::false_type{});
+    if constexpr (KIND == kLossLogits) {
+      auto main_loop = [&](auto iss_c) {
+        using Wait = std::integral_constant<int, 2 * DLOADS>;  // the loads of this step and the last one
+        const int nk = cur.nk, units = nk / 2;
+        if constexpr (decltype(iss_c)::value) LOSS_WAIT_VMCNT(4 * PL);
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int r = 0; r < NRD; ++r) {
+          if (r < MI) pf[0][r] = frag_p(0, r, 0, std::false_type{});
+          else qf[0][r - MI] = frag_w(kQAt, r - MI, 0);
+        }
+        int qs = 0;  // this pair's place of w
+        for (int u = 0; u < units; ++u) {
+          const int qn = qs == 2 ? 0 : qs + 1, qfar = qs == 0 ? 2 : qs - 1;
+          static_for<2>([&](auto hc) {
+            constexpr int h = decltype(hc)::value;
+            const int k = u * 2 + h, at = (k & 3) * HALF, an = ((k + 1) & 3) * HALF, af = ((k + 3) & 3) * HALF;
+            const int w1 = kQAt + qs * (2 * HALF), w0 = kQAt + (h ? qn : qs) * (2 * HALF);
+            step(iss_c, Wait{},
+                 [&](int r) {
+                   if (r < MI) pf[1][r] = frag_p(at, r, 1, std::false_type{});
+                   else qf[1][r - MI] = frag_w(w1, r - MI, h * 2 + 1);
+                 },
+                 [&](int r) {
+                   if (r < MI) pf[0][r] = frag_p(an, r, 0, std::false_type{});
+                   else qf[0][r - MI] = frag_w(w0, r - MI, h ? 0 : 2);
+                 },
+                 [&](int i) { issue_p(i, min(k + 3, nk - 1), af, std::false_type{}); },
+                 [&](int i) { issue_w(h * PL + i, min(u + 2, units - 1), kQAt + qfar * (2 * HALF)); });
+          });
+          qs = qn;
+        }
+      };
+      if (issuer) main_loop(std::true_type{});
+      else main_loop(std::false_type{});
+    } else {
+      auto main_loop = [&](auto iss_c, auto trans_c) {
+        using Wait = std::integral_constant<int, (kStages - 2) * DLOADS>;
+        const int nk = cur.nk, last = cur.k0 + nk - 1;
+        if constexpr (decltype(iss_c)::value) LOSS_WAIT_VMCNT((kStages - 2) * DLOADS);
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int r = 0; r < NRD; ++r) {
+          if (r < MI) pf[0][r] = frag_p(0, r, 0, trans_c);
+          else qf[0][r - MI] = frag_q(HALF, r - MI, 0, trans_c);
+        }
+        int cs = 0, ns = 1, fs = kStages - 1;  // stages of steps kt, kt + 1, kt + kStages - 1
+        for (int kt = 0; kt < nk; ++kt) {
+          const int kl = min(cur.k0 + kt + kStages - 1, last);
+          const int at = cs * STAGE, an = ns * STAGE, af = fs * STAGE;
+          step(iss_c, Wait{},
+               [&](int r) {
+                 if (r < MI) pf[1][r] = frag_p(at, r, 1, trans_c);
+                 else qf[1][r - MI] = frag_q(at + HALF, r - MI, 1, trans_c);
+               },
+               [&](int r) {
+                 if (r < MI) pf[0][r] = frag_p(an, r, 0, trans_c);
+                 else qf[0][r - MI] = frag_q(an + HALF, r - MI, 0, trans_c);
+               },
+               [&](int i) { issue_p(i, kl, af, trans_c); }, [&](int i) { issue_q(i, kl, af + HALF, trans_c); });
+          cs = ns;
+          ns = (ns + 1 == kStages) ? 0 : ns + 1;
+          fs = (fs + 1 == kStages) ? 0 : fs + 1;
+        }
+      };
+      auto by_op = [&](auto iss_c) {
+        if (b.g[cur.p].op == kLossDw) main_loop(iss_c, std::true_type{});
+        else main_loop(iss_c, std::false_type{});
+      };
+      if (issuer) by_op(std::true_type{});
+      else by_op(std::false_type{});
+    }
     // this tile's last loads have landed and its fragments are read before the next tile's loads reuse the stages
     LOSS_WAIT_VMCNT(0);
     __builtin_amdgcn_s_barrier();
-    if (has_next && issuer) prologue(nxt);  // (leaves stage kStages - 1 to the epilogue)
+    if (has_next && issuer) prologue(nxt);  // (leaves the last part of LDS to the epilogue)
     int after = -1;  // the item after that: asked for here, needed at the epilogue's end
     if (has_next && asks) after = take();
 
     // acc[mi][ni][4 gg + t] of a lane is element (row, column) of the wave's part with row = 32 mi + lane % 32,
     // column = 32 ni + 8 gg + 4 (lane / 32) + t.
-    lds_byte* slab = (lds_byte*)(smem + (kStages - 1) * STAGE);
+    lds_byte* slab = (lds_byte*)(smem + kSlabAt);
     int ln = lane;
     asm volatile("" : "+v"(ln));  // lane-dependent offsets are formed here, not kept through the main loop
     const int er = ln & 31, eh = ln >> 5;
@@ -494,18 +662,6 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   LOSS_WAIT_VMCNT(0);
 }
 
-// 32 rows x 256 columns of bf16 in LDS, as 16 x 32 blocks of swizzled 16-byte chunks; and one 16-byte piece of the
-// transposed block of columns 16 jp .. (lane: column lane % 16, rows 8 (lane / 16) ..).
-__device__ __forceinline__ int tile_off(int r, int c) {
-  return (((r >> 4) * 8 + (c >> 5)) << 10) + ((r & 15) << 6) + ((((c & 31) >> 3) ^ swz(r & 15)) << 4) + ((c & 7) << 1);
-}
-__device__ __forceinline__ u32x4 transposed_piece(lds_byte* tile, int jp, int ln) {
-  const int r = (ln >> 4) * 8 + ((ln >> 2) & 3), c = jp * 16 + (ln & 3) * 4;
-  const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)(tile + tile_off(r, c)));
-  const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)(tile + tile_off(r + 4, c)));
-  return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 // the next of an fp32 value's three bf16 parts; what is left of the values stays in x
 __device__ __forceinline__ u32x4 split8(float (&x)[8]) {
   u32x4 o;
@@ -597,8 +753,7 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
 }
 
 // One 32 x 256 tile of a packed operand: four 8-column chunks per thread (row it * 8 + t / 32, chunk t % 32).
-__device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, uint8_t* smem, int* counts) {
-  lds_byte* tile = (lds_byte*)smem;
+__device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, int* counts) {
   const int64_t i = int(blockIdx.x) - d.blocks_begin;
   const int64_t tc = d.cols / 256, r0 = i / tc * 32, c0 = i % tc * 256;
   const int t = threadIdx.x, ch = t & 31;
@@ -654,30 +809,19 @@ __device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, 
       }
     }
   }
-  const int ln = t & 63, w = t >> 6;
   for (int part = 0; part < (d.bf16 ? 1 : 3); ++part) {
-    if (part) __syncthreads();  // the last part's transposed reads are done
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
       const u32x4 v = split8(x[it]);
-      const int r = it * 8 + (t >> 5);
-      if (d.dst && c < d.ldn) *(gptr<u32x4>)(d.dst + part * d.dst_part + blk_index(r0 + r, c, d.ldn)) = v;
-      if (d.dst_t) *(lptr<u32x4>)(tile + tile_off(r, ch * 8)) = v;
-    }
-    if (d.dst_t) {
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int jp = w * 4 + j;
-        *(gptr<u32x4>)(d.dst_t + part * d.dst_t_part + blk_index(c0 + jp * 16 + (ln & 15), r0 + (ln >> 4) * 8, d.ldt)) =
-            transposed_piece(tile, jp, ln);
-      }
+      const int64_t r = r0 + it * 8 + (t >> 5);
+      uint16_t* dst = d.dst + part * d.dst_part;
+      if (d.blocked) *(gptr<u32x4>)(dst + blk_index(r, c, d.ld)) = v;
+      else if (r < d.R && c < d.ld) *(gptr<u32x4>)(dst + r * d.ld + c) = v;
     }
   }
 }
 
 __global__ __launch_bounds__(256) void loss_prep_kernel(const LossPrep a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
   __shared__ int counts[32];
   if (blockIdx.x == 0 && threadIdx.x < kLossQueues * kGemmXcds) a.queues[threadIdx.x] = 0;
   if (int(blockIdx.x) < a.label_blocks) {
@@ -685,7 +829,7 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(const LossPrep a) {
     if (r < a.n_pad) prep_labels(a, r);
     return;
   }
-  prep_pack(a, a.d[a.packs > 1 && int(blockIdx.x) >= a.d[1].blocks_begin ? 1 : 0], smem, counts);
+  prep_pack(a, a.d[a.packs > 1 && int(blockIdx.x) >= a.d[1].blocks_begin ? 1 : 0], counts);
 }
 
 // Sum over a workgroup, in 64 bits and a fixed order, of n values (times b where a value is not 0); for every thread.
@@ -784,12 +928,11 @@ __global__ __launch_bounds__(1024) void loss_total_kernel(const LossTotal a) {
 }
 
 // One 32 x 256 tile of dz per workgroup of 256: from the logits to LDS, the targets' elements there from their fp32 logits,
-// then out in both layouts. Bound by HBM: 2 bytes read and 4 written per logit (bf16).
+// then out. Bound by HBM: 2 bytes read and 2 written per logit (bf16).
 template <bool F32>
 __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[32 * 256 * 2];
-  __shared__ float fix[F32 ? 32 * 256 : 1];
-  lds_byte* tile = (lds_byte*)smem;
+  // chunk c of 8 columns of row r at r * 32 + (c ^ r) (fp32: two 16-byte halves, 32 chunks apart per row pair)
+  __shared__ __attribute__((aligned(16))) uint8_t smem[32 * 256 * (F32 ? 4 : 2)];
   const int tc = a.v_pad / 256;
   if (int64_t(blockIdx.x) == int64_t(a.rows_pad / 32) * tc) {  // (one more workgroup, for the loss)
     sum_loss<256>(a.total, (double*)smem);
@@ -797,10 +940,11 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   }
   const int64_t r0 = int64_t(blockIdx.x / tc) * 32, c0 = int64_t(blockIdx.x % tc) * 256;
   const int t = threadIdx.x, ln = t & 63, w = t >> 6;
-  // chunk (row, 8 columns) it of a thread: bf16 as its 1 KiB block lies (lane: row lane / 4, chunk lane % 4); fp32
-  // along the row
-  auto crow = [&](int it) { return F32 ? it * 8 + (t >> 5) : (it >> 1) * 16 + (ln >> 2); };
-  auto ccol = [&](int it) { return F32 ? (t & 31) * 8 : (w * 2 + (it & 1)) * 32 + (ln & 3) * 8; };
+  // chunk (row, 8 columns) it of a thread, as its 1 KiB block lies: lane: row lane / 4, chunk lane % 4
+  auto crow = [&](int it) { return (it >> 1) * 16 + (ln >> 2); };
+  auto ccol = [&](int it) { return (w * 2 + (it & 1)) * 32 + (ln & 3) * 8; };
+  auto at16 = [](int r, int c) { return r * 512 + (((c >> 3) ^ (r & 31)) << 4) + (c & 7) * 2; };
+  auto at32 = [](int r, int c) { return r * 1024 + (((c >> 2) ^ (r & 63)) << 4) + (c & 3) * 4; };
 #pragma unroll
   for (int it = 0; it < 4; ++it) {
     const int r = crow(it), cl = ccol(it);
@@ -814,8 +958,8 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         x[e] = rw.z != 0.0f && c + e < a.v ? expf((e < 4 ? v0[e & 3] : v1[e & 3]) - rw.x) * f : 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) fix[r * 256 + cl + e] = x[e];
+      *(lptr<f32x4_t>)(smem + at32(r, cl)) = f32x4_t{x[0], x[1], x[2], x[3]};
+      *(lptr<f32x4_t>)(smem + at32(r, cl + 4)) = f32x4_t{x[4], x[5], x[6], x[7]};
     } else {
       const u32x4 v = *(gptr<const u32x4>)(a.codes + blk_index(row, c, a.ldc));
       const float m = c < a.v ? a.gm[(c >> a.group_shift) * a.ldr + row] : 0.0f;
@@ -826,8 +970,8 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
         const float p = q == 65535u ? 0.0f : __builtin_amdgcn_exp2f(base - float(q) * (kLossOctaves / 65535.0f));
         x[e] = rw.z != 0.0f && c + e < a.v ? p * f : 0.0f;
       }
-      *(lptr<u32x4>)(tile + tile_off(r, cl)) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                     pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+      *(lptr<u32x4>)(smem + at16(r, cl)) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                 pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
     }
   }
   __syncthreads();
@@ -844,39 +988,21 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
     // p - q, from what is exact where both are near 1
     const float pq = e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * rw.y : e - q * (1.0f + rw.y);
     const float x = rw.z * (pq + rw.w * e) / (1.0f + rw.y);
-    if constexpr (F32)
-      fix[r * 256 + id] = x;
-    else
-      *(lptr<uint16_t>)(tile + tile_off(r, id)) = uint16_t(pack_bf16x2(x, 0.0f));
+    if constexpr (F32) *(lptr<float>)(smem + at32(r, id)) = x;
+    else *(lptr<uint16_t>)(smem + at16(r, id)) = uint16_t(pack_bf16x2(x, 0.0f));
   }
   __syncthreads();
-  for (int part = 0; part < (F32 ? 3 : 1); ++part) {
+#pragma unroll
+  for (int it = 0; it < 4; ++it) {
+    const int r = crow(it), cl = ccol(it);
+    uint16_t* dst = a.dz + blk_index(r0 + r, c0 + cl, a.ldc);
     if constexpr (F32) {
-      if (part) __syncthreads();
+      const f32x4_t v0 = *(lptr<f32x4_t>)(smem + at32(r, cl)), v1 = *(lptr<f32x4_t>)(smem + at32(r, cl + 4));
+      float x[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
 #pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        const int r = crow(it), cl = ccol(it);
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fix[r * 256 + cl + e];
-        const u32x4 v = split8(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) fix[r * 256 + cl + e] = x[e];
-        *(gptr<u32x4>)(a.dz + part * a.dz_part + blk_index(r0 + r, c0 + cl, a.ldc)) = v;
-        *(lptr<u32x4>)(tile + tile_off(r, cl)) = v;
-      }
-      __syncthreads();
+      for (int part = 0; part < 3; ++part) *(gptr<u32x4>)(dst + part * a.dz_part) = split8(x);
     } else {
-#pragma unroll
-      for (int it = 0; it < 4; ++it)
-        *(gptr<u32x4>)(a.dz + blk_index(r0 + crow(it), c0 + ccol(it), a.ldc)) = *(lptr<u32x4>)(tile + tile_off(crow(it), ccol(it)));
-    }
-    if (!a.dz_t) continue;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int jp = w * 4 + j;
-      *(gptr<u32x4>)(a.dz_t + part * a.dz_t_part + blk_index(c0 + jp * 16 + (ln & 15), r0 + (ln >> 4) * 8, a.ldt)) =
-          transposed_piece(tile, jp, ln);
+      *(gptr<u32x4>)dst = *(lptr<u32x4>)(smem + at16(r, cl));
     }
   }
 }
@@ -1003,9 +1129,9 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
           const int grp = lane >> 4, i = lane & 15, row = sl * 16 + (grp >> 1) * 8 + (i >> 2);
           const int sl16 = w * 4 + (grp & 1) * 2 + ((i & 3) >> 1);
           lds_byte* q = (lds_byte*)(smem + cs * STAGE + PB) + row * 512 + ((sl16 ^ ((row & 3) << 1)) << 4) + (i & 1) * 8;
-          const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)q);
-          const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lptr<bf16x4_t>)(q + 4 * 512));
-          qf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          const bf16x4_t lo = read_tr((lptr<bf16x4_t>)q);
+          const bf16x4_t hi = read_tr((lptr<bf16x4_t>)(q + 4 * 512));
+          qf = join_tr(lo, hi);
         }
 #pragma unroll
         for (int i = 0; i < MI; ++i) {

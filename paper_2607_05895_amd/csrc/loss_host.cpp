@@ -2,15 +2,15 @@
 // stream, descriptors as kernel arguments).
 //
 //   per chunk of rows of x (usually one):
-//     prep    the labels in one form (first chunk); x's rows and (first chunk) w as panel-blocked bf16, and transposed where a
-//             gradient reads them so
+//     prep    the labels in one form (first chunk); x's rows as panel-blocked bf16; a bf16 copy of w where it cannot be read as
+//             it lies (first chunk)
 //     logits  z = x w^T: per row and 64 columns the softmax partials, the targets' logits and (for gradients) the logits
 //     rows    the partials joined: the tokens' losses, and the weights of their gradients; with MEAN (first chunk) the weights'
 //             sum
-//     grad    dz, in both layouts; (last chunk) the loss
+//     grad    dz in the logits' place; (last chunk) the loss
 //     dx      dz w            (K ranges and their join where there are few tiles)
 //     dw      dz^T x          (added to the earlier chunks' sum, held in fp32; in one launch with dx where both are small)
-// For a few tokens and bf16 the logits and dx read w as it lies instead of a packed copy.
+// For a few tokens the logits and dx run on kernels that read w once at HBM's rate.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,19 +50,20 @@ struct Gemm {
 
 struct Plan {
   bool f32 = false, grads = false;
-  int stream = 0;               // rows / 32 of the products that read w as it lies, or 0
+  bool copy = false;            // w is read from a bf16 copy
+  int stream = 0;               // rows / 32 of the products for a few tokens, or 0
   int parts = 1, nseg = 1;
   int64_t n = 0, v = 0, h = 0, k = 1;
-  int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0;
+  int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0, ldw = 0;
   int group = kLossGroup;       // columns of a softmax partial
   Gemm logits, dx, dw;
   // offsets
   size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, queues = 0, row = 0, zt = 0, gm = 0, gs = 0;
-  size_t xb = 0, xt = 0, wb = 0, wt = 0, codes = 0, z32 = 0, dz_t = 0, part = 0, acc = 0;
+  size_t xb = 0, wb = 0, codes = 0, z32 = 0, part = 0, acc = 0;
   size_t bytes = 0;
 };
 
-// Most tokens whose products read w as it lies, and the fewest ids.
+// The most tokens, and the fewest ids, of the products for a few tokens.
 constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
 
 // A launch's time in us on `tile` x `tile` tiles, items[i] of steps[i] K steps each: what the chip's workgroups share, or the
@@ -160,7 +161,9 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.vp = up(p.v, 256);
   p.hk = up(p.h, 64);
   p.hp = up(p.h, 256);
-  if (!p.f32 && p.n > 0 && p.n <= kStreamTokens && p.h % 8 == 0 && p.v >= kStreamIds) {
+  p.copy = p.f32 || p.h % 8 != 0;
+  p.ldw = p.copy ? p.hk : p.h;
+  if (!p.copy && p.n > 0 && p.n <= kStreamTokens && p.v >= kStreamIds) {
     p.stream = p.n <= 32 ? 1 : p.n <= 64 ? 2 : 4;
     p.group = 32;
     p.chunk = p.n_pad = 32 * p.stream;
@@ -218,15 +221,12 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.zt = take(p.chunk * k * 4);
   p.gm = take(groups * p.chunk * 4);
   p.gs = take(groups * p.chunk * 4);
-  p.xb = take(p.chunk * p.hk * es);
-  if (!p.stream) p.wb = take(p.vp * p.hk * es);
-  if (a->dw) p.xt = take(p.hp * p.chunk * es);
-  if (a->dx && !p.stream) p.wt = take(p.hp * p.vp * es);
+  p.xb = take(p.chunk * p.hp * es);
+  if (p.copy) p.wb = take(p.v * p.ldw * es);
   if (p.grads) {
     p.codes = take(p.chunk * p.vp * es);
     if (p.f32) p.z32 = take(p.chunk * p.vp * 4);
   }
-  if (a->dw) p.dz_t = take(p.vp * p.chunk * es);
   p.part = take(int64_t(part));
   if (a->dw && p.chunk < p.n) p.acc = take(p.vp * p.hp * 4);
   p.bytes = o;
@@ -272,21 +272,19 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
   prep.ent = f32p(p.ent);
   prep.on = f32p(p.on);
 
-  const int64_t xpart = p.chunk * p.hk, xtpart = p.hp * p.chunk, wpart = p.vp * p.hk, wtpart = p.hp * p.vp;
-  const int64_t dzpart = p.chunk * p.vp;
-  // part pairs, the small products first: they are added while the sum is small
-  static const int kPair[kLossMaxSeg][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
-  auto product = [&](const Gemm& g, size_t P, int64_t ldp, int64_t ppart, size_t Q, int64_t ldq, int64_t qpart, int nk) {
+  const int64_t xpart = p.chunk * p.hp, wpart = p.v * p.ldw, dzpart = p.chunk * p.vp;
+  const uint16_t* const w = p.copy ? u16p(p.wb) : static_cast<const uint16_t*>(a->w);
+  // P Q^T with Q = w (row-major) or x (panel blocked)
+  auto product = [&](const Gemm& g, size_t P, int64_t ldp, int64_t ppart, bool of_w, int nk) {
     LossGemm m{};
     m.P = u16p(P);
-    m.Q = u16p(Q);
     m.ldp = ldp;
-    m.ldq = ldq;
+    m.ppart = ppart;
+    m.Q = of_w ? w : u16p(p.xb);
+    m.ldq = of_w ? p.ldw : p.hp;
+    m.qrows = p.v;
+    m.qpart = of_w ? wpart : xpart;
     m.nseg = p.nseg;
-    for (int s = 0; s < p.nseg && p.nseg > 1; ++s) {
-      m.pseg[s] = kPair[s][0] * ppart;
-      m.qseg[s] = kPair[s][1] * qpart;
-    }
     m.nk = nk;
     m.kper = g.splits > 1 ? g.kper : p.nseg * nk;
     m.splits = (p.nseg * nk + m.kper - 1) / m.kper;
@@ -303,34 +301,30 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     prep.label_blocks = first ? int((p.n_pad + 3) / 4) : 0;
     prep.packs = 0;
     int blocks = prep.label_blocks;
-    auto pack = [&](const void* src, int64_t R, int64_t rpad, size_t dst, int64_t part, bool with_t, size_t dst_t,
-                    int64_t ldt, int64_t tpart, int64_t label_row) {
+    auto pack = [&](const void* src, int64_t R, int64_t rpad, size_t dst, int64_t ld, int64_t part, int64_t label_row) {
       LossPack& d = prep.d[prep.packs++];
       d.src = src;
       d.R = R;
       d.C = p.h;
       d.dst = u16p(dst);
-      d.ldn = p.hk;
+      d.ld = ld;
       d.dst_part = part;
-      d.dst_t = with_t ? u16p(dst_t) : nullptr;
-      d.ldt = ldt;
-      d.dst_t_part = tpart;
       d.cols = p.hp;
       d.label_row = label_row;
       d.blocks_begin = blocks;
       d.bf16 = !p.f32;
+      d.blocked = label_row >= 0;
       blocks += int(rpad / 32 * (p.hp / 256));
     };
-    pack(static_cast<const uint8_t*>(a->x) + r0 * p.h * es, rows, rows_pad, p.xb, xpart, a->dw != nullptr, p.xt, p.chunk,
-         xtpart, r0);
-    if (first && !p.stream) pack(a->w, p.v, p.vp, p.wb, wpart, a->dx != nullptr, p.wt, p.vp, wtpart, -1);
+    pack(static_cast<const uint8_t*>(a->x) + r0 * p.h * es, rows, rows_pad, p.xb, p.hp, xpart, r0);
+    if (first && p.copy) pack(a->w, p.v, up(p.v, 32), p.wb, p.ldw, wpart, -1);
     LOSS_TRY(launch_loss_prep(prep, blocks, st), "prep launch");
 
     if (p.stream) {
       LossStream z{};
       z.P = u16p(p.xb);
-      z.w = static_cast<const uint16_t*>(a->w);
-      z.ldp = p.hk;
+      z.w = w;
+      z.ldp = p.hp;
       z.v = p.v;
       z.h = p.h;
       z.nk = int(p.hk / 64);
@@ -350,7 +344,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     } else {
       LossGemm2 zz{};
       LossGemm& z = zz.g[0];
-      z = product(p.logits, p.xb, p.hk, xpart, p.wb, p.hk, wpart, p.logits.nk);
+      z = product(p.logits, p.xb, p.hp, xpart, true, p.logits.nk);
       zz.count = 1;
       zz.queue = prep.queues;
       z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
@@ -404,10 +398,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     gr.logits = p.f32 ? f32p(p.z32) : nullptr;
     gr.ldc = p.vp;
     gr.dz = u16p(p.codes);
-    gr.dz_t = a->dw ? u16p(p.dz_t) : nullptr;
     gr.dz_part = dzpart;
-    gr.dz_t_part = dzpart;
-    gr.ldt = p.chunk;
     gr.gm = rw.gm;
     gr.ldr = p.chunk;
     gr.row = rw.row;
@@ -425,7 +416,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
 
     LossGemm mx{}, mw{};
     if (a->dx && !p.stream) {
-      mx = product(p.dx, p.codes, p.vp, dzpart, p.wt, p.vp, wtpart, p.dx.nk);
+      mx = product(p.dx, p.codes, p.vp, dzpart, true, p.dx.nk);
+      mx.op = kLossDx;
       mx.tm = int(up(rows, p.dx.tile) / p.dx.tile);
       mx.rows = int(rows);
       mx.cols = int(p.h);
@@ -437,7 +429,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (mx.splits > 1) mx.part = f32p(p.part);
     }
     if (a->dw) {
-      mw = product(p.dw, p.dz_t, p.chunk, dzpart, p.xt, p.chunk, xtpart, int(up(rows, 32) / 32));
+      mw = product(p.dw, p.codes, p.vp, dzpart, false, int(up(rows, 32) / 32));
+      mw.op = kLossDw;
       mw.rows = int(p.v);
       mw.cols = int(p.h);
       mw.out = a->dw;
@@ -455,7 +448,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     if (a->dx && p.stream) {
       LossStream s{};
       s.P = u16p(p.codes);
-      s.w = static_cast<const uint16_t*>(a->w);
+      s.w = w;
       s.ldp = p.vp;
       s.v = p.v;
       s.h = p.h;

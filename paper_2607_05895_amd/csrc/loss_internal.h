@@ -1,11 +1,10 @@
 // Descriptors and launchers of the losses over a vocabulary (loss_host.cpp, kernels_loss.hip).
 //
 // For n tokens with hidden states x (n x h) and a head w (v x h), in chunks of rows of x:
-//   z = x w^T / T            logits     P = x,   Q = w,    K = h
-//   dx = dz w                           P = dz,  Q = w^T,  K = v
-//   dw = dz^T x                         P = dz^T, Q = x^T, K = the chunk's rows
-// Every operand is bf16, panel blocked (blk_index), zero padded: rows to the tile, K to a whole number of steps. An fp32
-// tensor is held in three bf16 parts, and a product runs over six pairs of parts, one K segment each.
+//   z = x w^T / T    logits       dx = dz w       dw = dz^T x
+// x and dz are bf16, panel blocked (blk_index), zero padded (rows to the tile, columns to 256); w is read as it lies, row-major,
+// or, where it is fp32 or its rows are no multiple of 16 bytes, from a row-major bf16 copy. An fp32 tensor is held in three bf16
+// parts, and a product runs over six pairs of parts, one K segment each.
 //
 // Between the logits and their gradient a chunk of bf16 inputs holds each logit in 16 bits: the distance
 // from the largest of its row in its 64 columns, in steps of 64 / 65535 of a factor of two. That is a relative error of p of
@@ -29,15 +28,17 @@ constexpr int kLossQueues = 3;         // launches of products per chunk that ta
 constexpr int kLossMaxTop = 256;     // most teacher logits a token
 constexpr float kLossOctaves = 64.0f;  // factors of two that the 16-bit codes of the logits span
 
-// One NT product over panel-blocked operands: tiles of P Q^T, K in nseg segments (part pairs) of nk steps of 32, cut
-// into `splits` ranges of kper steps.
+// One product: tiles of P Q^T, K in nseg segments (pairs of parts) of nk steps of 32, cut into `splits` ranges of kper steps.
+// P is panel blocked, and so is dw's Q (x); the others' Q is w, row-major with qrows rows.
+enum { kLossDx = 0, kLossDw = 1 };
 struct LossGemm {
   const uint16_t *P, *Q;
-  int64_t ldp, ldq;                                // K columns of the buffers
-  int64_t pseg[kLossMaxSeg], qseg[kLossMaxSeg];    // element offsets of each segment's parts
+  int64_t ldp, ldq, qrows;
+  int64_t ppart, qpart;                            // elements between the parts
   int32_t nseg, nk, splits, kper;
   int32_t tm, tn;                                  // tiles
   int32_t rows, cols;                              // real rows and columns of the result
+  int32_t op;                                      // kLossDx, kLossDw (gradients)
   // logits: softmax partials per row and 64 columns, the targets' logits, and the logits themselves (or none of them)
   float inv_t;
   float *gm, *gs;                                  // [group][ldr]: largest logit; sum of the others' exp relative to it
@@ -92,16 +93,17 @@ struct LossLabels {
   float inv_t;
 };
 
-// Panel-blocked bf16 copies of a row-major R x C matrix: as it is (dst, ldn columns) and transposed (dst_t, ldt columns),
-// in `parts` parts (1: bf16 source; 3: fp32 source) that lie dst_part (dst_t_part) elements apart.
+// A bf16 copy of a row-major R x C matrix, in one part (bf16 source) or three (fp32 source) that lie dst_part elements
+// apart: panel blocked with ld columns, padded with zeros to the launch's rows and ld, or row-major with ld columns.
 struct LossPack {
   const void* src;
   int64_t R, C;
-  uint16_t *dst, *dst_t;
-  int64_t ldn, ldt, dst_part, dst_t_part;
-  int64_t cols;                // padded columns (a multiple of 256)
+  uint16_t* dst;
+  int64_t ld, dst_part;
+  int64_t cols;                // columns that the launch covers (a multiple of 256)
   int64_t label_row;           // the label of row 0 (rows whose token does not count are written as zeros), or -1: all rows
   int32_t blocks_begin, bf16;  // first workgroup
+  int32_t blocked;
 };
 
 // The first launch: the labels in one form (per token k ids with weights q that add up to 1, -1 and 0 for none; the sum of
@@ -144,14 +146,14 @@ struct LossRows {
 };
 
 // dz of a chunk, without the factor scale / (T D) common to all tokens (which the products apply: rounded with it, the
-// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place and transposed, or fp32
-// logits -> three bf16 parts and their transposes.
+// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place, or fp32
+// logits -> three bf16 parts.
 struct LossGrad {
   uint16_t* codes;
   const float* logits;
   int64_t ldc;
-  uint16_t *dz, *dz_t;         // (codes: dz = codes)
-  int64_t dz_part, dz_t_part, ldt;
+  uint16_t* dz;                // (codes: dz = codes)
+  int64_t dz_part;
   const float* gm;
   int64_t ldr;
   const float4* row;
