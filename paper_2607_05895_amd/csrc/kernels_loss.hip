@@ -854,10 +854,10 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
   m = hi;
 }
 
-// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB, four at a time.
+// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB, BATCH at a time.
 template <int RPB>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
-  constexpr int GS = 1024 / RPB;
+  constexpr int GS = 1024 / RPB, BATCH = RPB == 4 ? 16 : 8;
   __shared__ float sm[GS][RPB + 1], ss[GS][RPB + 1];
   __shared__ double part[16];
   const int blocks = a.rows_pad / RPB;
@@ -869,16 +869,21 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
     const int64_t r = int64_t(blockIdx.x) * RPB + rl;
     const float none = -__builtin_inff();
     float m = none, s = 0.0f;
-    for (int g = gl; g < a.groups; g += 4 * GS) {
-      float gm[4], gs[4];
+    // (asked for here, needed at the end)
+    const bool mine = gl == 0 && r < a.rows;
+    const float on = mine ? a.on[r] : 0.0f, ent = mine ? a.ent[r] : 0.0f, wt = mine && a.weight ? a.weight[r] : 1.0f;
+    const float q0 = mine ? a.q[r * a.k] : 0.0f, z0 = mine ? a.zt[r * a.k] : 0.0f;
+    const int id0 = mine ? a.id[r * a.k] : -1;
+    for (int g = gl; g < a.groups; g += BATCH * GS) {
+      float gm[BATCH], gs[BATCH];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < BATCH; ++i) {
         const bool in = g + i * GS < a.groups;
         gm[i] = in ? a.gm[(g + i * GS) * a.ldr + r] : none;
         gs[i] = in ? a.gs[(g + i * GS) * a.ldr + r] : 0.0f;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) join_softmax(m, s, gm[i], gs[i]);
+      for (int i = 0; i < BATCH; ++i) join_softmax(m, s, gm[i], gs[i]);
     }
     sm[gl][rl] = m;
     ss[gl][rl] = s;
@@ -895,18 +900,16 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
       if (r >= a.rows) {
         a.row[r] = float4{0.0f, 0.0f, 0.0f, 0.0f};
       } else {
-        const float on = a.on[r];
         const float ls = log1pf(s), lse = m + ls;
         float loss = 0.0f;
         if (on != 0.0f) {
-          float d = a.ent[r];
-          for (int j = 0; j < a.k; ++j) {
+          float d = ent + (q0 > 0.0f && id0 >= 0 ? q0 * (m - z0) : 0.0f);
+          for (int j = 1; j < a.k; ++j) {
             const float q = a.q[r * a.k + j];
             if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (m - a.zt[r * a.k + j]);
           }
           loss = (d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
         }
-        const float wt = on != 0.0f ? (a.weight ? a.weight[r] : 1.0f) : 0.0f;
         a.row[r] = float4{m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
         if (a.token_loss) a.token_loss[r] = loss;
         if (a.lse) a.lse[r] = on != 0.0f ? lse : 0.0f;
@@ -1049,27 +1052,33 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
   store4(a.out, a.out_bf16, int64_t(row) * a.ldo + c, s, a.cols - c);
 }
 
-// Products for at most 32 MI tokens with w as it lies (LossStream). Eight waves, each all rows by 32 of the tile's 256
-// columns; K in steps of 64 through a ring of NST stages filled NST - 1 steps ahead by direct loads. Bound by HBM: w is read
-// once, 32 KiB per step, with up to (NST - 1) steps of it in flight per CU.
-// logits: a stage holds 256 rows of w by 64 of h (128-byte rows of eight 16-byte chunks, chunk c of row r in slot c ^ (r / 2) % 8).
-// dx: 64 rows of w by 256 of h (512-byte rows, chunk c in slot c ^ 2 (r % 4)), its fragments read transposed.
+// Products for at most 32 MI tokens (LossStream). Eight waves; K in steps through a ring of NST stages filled NST - 1 steps
+// ahead by direct loads. Bound by HBM: w is read once, 32 KiB per step, with up to (NST - 1) steps of it in flight per CU.
+// logits: a stage holds QR rows of w by KT of h; a wave takes all tokens by 32 rows of w, and half of the step's K where QR = 128
+//   (the halves are added in LDS at the tile's end). 128 rows of 256 bytes rather than 256 of 128: a head of 128256 x 4096 is read
+//   in 215 us (4.9 TB/s) instead of 227; more tokens leave no room for it.
+// dx: 64 rows of w by 256 of h, a wave 32 columns; chunk c of row r in slot c ^ 2 (r % 4); fragments read transposed.
 // Past a row's end lie the next row's values, past w's end its last ones: they meet zeros of x or dz, or belong to columns
 // that are not stored.
 template <int MI, int KIND>
 __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a) {
-  constexpr int PB = MI * 32 * 128, QB = 256 * 128, STAGE = PB + QB;
-  constexpr int NST = MI <= 2 ? 4 : 3;
-  constexpr int PL = MI < 2 ? 1 : MI / 2, LOADS = PL + 4;  // per wave and step (MI = 1: two waves load the same)
-  static_assert(NST * STAGE <= 160 * 1024, "LDS");
+  constexpr int QR = stream_rows(MI), KT = KIND == kLossLogits ? 16384 / QR : 64;  // (dx: QR is not used)
+  constexpr int KB = KT / 32, PB = MI * 32 * KT * 2, QB = 32768, STAGE = PB + QB;
+  constexpr int NST = 160 * 1024 / STAGE < 4 ? 160 * 1024 / STAGE : 4;
+  constexpr int PBLK = MI * 2 * KB;                            // 1 KiB blocks of P per step
+  constexpr int PL = PBLK < 8 ? 1 : PBLK / 8, LOADS = PL + 4;  // per wave and step (four blocks: two waves load the same)
+  static_assert(NST >= 2 && NST * STAGE <= 160 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[NST * STAGE];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int total = a.tiles * a.splits;
   const int64_t wrow = a.h * 2;  // bytes
   const uint32_t ploff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
+  constexpr int LPR = KT / 8, RPI = 64 / LPR;  // logits: lanes per row of w, rows per load
+  const int qr = w * RPI + lane / LPR;         // this lane's row of its first load (later ones: 8 RPI further, the same swizzle)
+  const int qsw = KT == 64 ? (qr >> 1) & 7 : qr & 15;
   const uint32_t qloff = KIND == kLossLogits
-                             ? uint32_t((lane >> 3) * wrow) + ((lane & 7) ^ (((w & 1) * 4 + (lane >> 4)) & 7)) * 16
-                             : uint32_t((lane >> 5) * wrow) + ((lane & 31) ^ (((w & 1) * 2 + (lane >> 5)) << 1)) * 16;
+                             ? uint32_t(qr * wrow) + ((lane % LPR) ^ qsw) * 16
+                             : uint32_t((w * 2 + (lane >> 5)) * wrow) + ((lane & 31) ^ (((w & 1) * 2 + (lane >> 5)) << 1)) * 16;
   // w from row r0 on; its loads are held to its last 16 bytes (whole chunks are in or out: h is a multiple of 8)
   uint32_t qmost = 0;
   auto rows_from = [&](int64_t r0) {
@@ -1079,23 +1088,25 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
   };
   auto issue = [&](int tile, int k, int stage) {
     lds_byte* sb = (lds_byte*)(smem + stage * STAGE);
-    const __amdgpu_buffer_rsrc_t pr = __builtin_amdgcn_make_buffer_rsrc((void*)a.P, 0, 0x7fffffff, 0x00020000);
+    const __amdgpu_buffer_rsrc_t pr = __builtin_amdgcn_make_buffer_rsrc((void*)a.P, 0, 0xffffffffu, 0x00020000);
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      const int b = (i * 8 + w) % (MI * 4), kb = b / (MI * 2), panel = b % (MI * 2);  // K half, 16-row panel
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, sb + kb * (PB / 2) + panel * 1024, 16, ploff,
-                                               uint32_t(panel) * uint32_t(a.ldp * 32) + uint32_t(k * 2 + kb) * 1024u, 0, 0);
+      const int b = (i * 8 + w) % PBLK, kb = b / (MI * 2), panel = b % (MI * 2);  // K block of 32, 16-row panel
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, sb + kb * (MI * 2048) + panel * 1024, 16, ploff,
+                                               uint32_t(panel) * uint32_t(a.ldp * 32) + uint32_t(k * KB + kb) * 1024u, 0, 0);
     }
-    const __amdgpu_buffer_rsrc_t qr = rows_from(KIND == kLossLogits ? int64_t(tile) * 256 : int64_t(k) * 64);
+    const __amdgpu_buffer_rsrc_t qr = rows_from(KIND == kLossLogits ? int64_t(tile) * QR : int64_t(k) * 64);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {  // logits: rows 8 (8 i + w) .. + 7; dx: rows 2 (8 i + w), + 1
-      const uint32_t at = KIND == kLossLogits ? uint32_t((i * 8 + w) * 8 * wrow) + uint32_t(k) * 128u
-                                              : uint32_t((i * 8 + w) * 2 * wrow) + uint32_t(tile) * 512u;
+    for (int i = 0; i < 4; ++i) {  // logits: rows RPI (8 i + w) ..; dx: rows 2 (8 i + w), + 1
+      const uint32_t at = KIND == kLossLogits ? uint32_t(i * 8 * RPI * wrow) + uint32_t(k) * uint32_t(KT * 2)
+                                              : uint32_t(i * 16 * wrow) + uint32_t(tile) * 512u;
       const uint32_t off = qloff + at;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, sb + PB + (i * 8 + w) * 1024, 16, off < qmost ? off : qmost, 0, 0, 0);
     }
   };
   const int fr = lane & 31, fh = lane >> 5;
+  constexpr int CB = QR / 32;  // logits: waves along w's rows
+  const int cb = KIND == kLossLogits ? w % CB : w, kh = KIND == kLossLogits ? w / CB : 0;
   int item = blockIdx.x;
   if (item >= total) return;
   auto range = [&](int it, int& k0, int& nk) {
@@ -1120,11 +1131,12 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
       issue(tile, k0 + min(kt + NST - 1, nk - 1), cs == 0 ? NST - 1 : cs - 1);
       const uint8_t* sb = smem + cs * STAGE;
 #pragma unroll
-      for (int sl = 0; sl < 4; ++sl) {  // 16 of K
+      for (int s4 = 0; s4 < 4; ++s4) {  // 16 of K
+        const int sl = kh * 4 + s4;
         bf16x8_t qf;
         if constexpr (KIND == kLossLogits) {
-          const int row = w * 32 + fr, c = sl * 2 + fh;
-          qf = *reinterpret_cast<const bf16x8_t*>(sb + PB + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
+          const int row = cb * 32 + fr, c = sl * 2 + fh;
+          qf = *reinterpret_cast<const bf16x8_t*>(sb + PB + row * (KT * 2) + ((c ^ (KT == 64 ? (row >> 1) & 7 : row & 15)) << 4));
         } else {
           const int grp = lane >> 4, i = lane & 15, row = sl * 16 + (grp >> 1) * 8 + (i >> 2);
           const int sl16 = w * 4 + (grp & 1) * 2 + ((i & 3) >> 1);
@@ -1135,7 +1147,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
         }
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-          const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(sb + (sl >> 1) * (PB / 2) + (i * 32 + fr) * kRowB +
+          const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(sb + (sl >> 1) * (MI * 2048) + (i * 32 + fr) * kRowB +
                                                                  ((((sl & 1) * 2 + fh) ^ swz(fr)) << 4));
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, pf, acc[i], 0, 0, 0);
         }
@@ -1154,9 +1166,30 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
     }
     // acc[i][4 g + t]: row 32 i + lane % 32, column 8 g + 4 (lane / 32) + t of the wave's 32
     if constexpr (KIND == kLossLogits) {
-      const int c0 = done * 256 + w * 32, left = int(a.v) - c0;
+      if constexpr (CB < 8) {  // the K halves' sums, through the stage that the next tile's first loads leave free
+        f32x4_t* half = reinterpret_cast<f32x4_t*>(smem + (NST - 1) * STAGE) + (cb * MI * 4) * 64 + lane;
+        static_assert(CB * MI * 4096 <= STAGE, "the halves' room");
+        if (kh) {
+#pragma unroll
+          for (int q = 0; q < MI * 4; ++q) {
+            const f32x16_t& c = acc[q >> 2];
+            half[q * 64] = f32x4_t{c[4 * (q & 3)], c[4 * (q & 3) + 1], c[4 * (q & 3) + 2], c[4 * (q & 3) + 3]};
+          }
+        }
+        LOSS_WAIT_LGKM0();
+        __builtin_amdgcn_s_barrier();
+        if (!kh) {
+#pragma unroll
+          for (int q = 0; q < MI * 4; ++q) {
+            const f32x4_t c = half[q * 64];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[q >> 2][4 * (q & 3) + t] += c[t];
+          }
+        }
+      }
+      const int c0 = done * QR + cb * 32, left = int(a.v) - c0;
       const float L = kLog2e * a.inv_t;
-      if (left > 0) {
+      if (left > 0 && !kh) {
         static_for<MI>([&](auto mi_c) {
           constexpr int mi = decltype(mi_c)::value;
           const int row = mi * 32 + fr;
@@ -1215,6 +1248,98 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
     if (!more) break;
   }
   LOSS_WAIT_VMCNT(0);
+}
+
+// dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). Many small workgroups instead of the
+// persistent kernel, whose tiles would each wait for one short load and one store after the other (48 tokens, 128256 x 4096: 247 us
+// for 1.05 GB, 295 there): four waves on 64 rows (ids) by 256 columns, all of K loaded at once, dz and x read transposed, the result through
+// LDS so that a wave stores whole rows of 512 bytes.
+template <int KS>
+__global__ __launch_bounds__(256) void loss_dw_kernel(const LossGemm a) {
+  constexpr int NPAN = 2 * KS, PB = NPAN * 2048, QB = NPAN * 8192;  // panels of 16 tokens; dz and x in LDS
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[PB + QB > 32768 ? PB + QB : 32768];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bj = blockIdx.x % a.tn, bi = blockIdx.x / a.tn;
+  const uint32_t loff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
+  const __amdgpu_buffer_rsrc_t pr =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(a.P + int64_t(bi) * 1024), 0, 0xffffffffu, 0x00020000);
+  const __amdgpu_buffer_rsrc_t qr =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(a.Q + int64_t(bj) * 4096), 0, 0xffffffffu, 0x00020000);
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {  // dz: panel b / 2, block b % 2
+    const int b = i * 4 + w;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, (lds_byte*)(smem + b * 1024), 16, loff,
+                                             uint32_t(b >> 1) * uint32_t(a.ldp * 32) + (b & 1) * 1024, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < NPAN * 2; ++i) {  // x: panel b / 8, block b % 8
+    const int b = i * 4 + w;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_byte*)(smem + PB + b * 1024), 16, loff,
+                                             uint32_t(b >> 3) * uint32_t(a.ldq * 32) + (b & 7) * 1024, 0, 0);
+  }
+  const float f = out_factor(a.alpha, a.denom);
+  f32x16_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+  const int trow = (lane >> 5) * 8 + ((lane >> 2) & 3), tchunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1), tbyte = (lane & 1) * 8;
+  const int tlo = trow * kRowB + ((tchunk ^ swz(trow)) << 4) + tbyte;
+  const int thi = (trow + 4) * kRowB + ((tchunk ^ swz(trow + 4)) << 4) + tbyte;
+  auto frag = [&](int at) {
+    lds_byte* q = (lds_byte*)(smem + at);
+    return join_tr(read_tr((lptr<bf16x4_t>)(q + tlo)), read_tr((lptr<bf16x4_t>)(q + thi)));
+  };
+  LOSS_WAIT_VMCNT(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int s = 0; s < NPAN; ++s) {
+    bf16x8_t pf[2], qf[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) pf[i] = frag((s * 2 + i) * 1024);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) qf[j] = frag(PB + (s * 8 + w * 2 + j) * 1024);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], pf[i], acc[i][j], 0, 0, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();  // (the fragments are read: the products need them)
+  // 64 rows of 512 bytes, 16-byte slots XORed by the row
+  const int er = lane & 31, eh = lane >> 5;
+  auto at = [](int r, int sl) { return r * 512 + ((sl ^ r) & 31) * 16; };
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const f32x16_t& v = acc[i][p >> 2];
+      const int o = 4 * (p & 3);
+      *(lptr<u32x2>)((lds_byte*)smem + at(i * 32 + er, w * 8 + (p >> 2) * 4 + (p & 3)) + eh * 8) =
+          u32x2{pack_bf16x2(v[o] * f, v[o + 1] * f), pack_bf16x2(v[o + 2] * f, v[o + 3] * f)};
+    }
+  LOSS_WAIT_LGKM0();
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int it = 0; it < 8; ++it) {
+    const int r = w * 16 + it * 2 + eh;
+    const u32x4 val = *(lptr<u32x4>)((lds_byte*)smem + at(r, er));
+    const int row = bi * 64 + r, c = bj * 256 + er * 8;
+    if (row < a.rows) {
+      uint16_t* dst = (uint16_t*)a.out + int64_t(row) * a.ldo + c;
+      if (c + 8 <= a.cols) {
+        *(gptr<u32x4_a2>)dst = val;
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (c + t < a.cols) *(gptr<uint16_t>)(dst + t) = uint16_t(val[t >> 1] >> (16 * (t & 1)));
+      }
+    }
+  }
 }
 
 // The K ranges' row-major results added in order: four columns per thread.
@@ -1333,6 +1458,14 @@ void launch_stream(const LossStream& a, int mi, hipStream_t st) {
   if (mi == 1) hipLaunchKernelGGL((loss_stream_kernel<1, KIND>), grid, block, 0, st, a);
   else if (mi == 2) hipLaunchKernelGGL((loss_stream_kernel<2, KIND>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((loss_stream_kernel<4, KIND>), grid, block, 0, st, a);
+}
+
+hipError_t launch_loss_dw(const LossGemm& a, int steps, hipStream_t st) {
+  const dim3 grid(unsigned((a.rows + 63) / 64) * unsigned(a.tn)), block(256);
+  if (steps == 1) hipLaunchKernelGGL(loss_dw_kernel<1>, grid, block, 0, st, a);
+  else if (steps == 2) hipLaunchKernelGGL(loss_dw_kernel<2>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(loss_dw_kernel<4>, grid, block, 0, st, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_loss_stream(const LossStream& a, int mi, int kind, hipStream_t st) {

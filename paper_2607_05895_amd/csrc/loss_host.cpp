@@ -327,8 +327,9 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       z.ldp = p.hp;
       z.v = p.v;
       z.h = p.h;
-      z.nk = int(p.hk / 64);
-      z.tiles = int(p.vp / 256);
+      const int qrows = stream_rows(p.stream), kt = 16384 / qrows;
+      z.nk = int(up(p.h, kt) / kt);
+      z.tiles = int(up(p.v, qrows) / qrows);
       z.splits = 1;
       z.kper = z.nk;
       z.inv_t = inv_t;
@@ -442,8 +443,11 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (!last) mw.part = f32p(p.acc);
     }
     LossGemm2 both{};
-    // one launch where both use the same tile; the longer tiles first
-    const bool together = a->dx && a->dw && !p.stream && p.dx.tile == p.dw.tile;
+    // dw of a few tokens on a kernel of its own (48 tokens, 128256 x 4096: 247 us, 295 on the tiles' kernel), unless its tiles go into
+    // dx's launch in one round (64 tokens, 1000 x 64, dx and dw: 13 us in one launch, 20 in two)
+    const bool short_dw = !p.f32 && first && last && rows <= kStreamTokens && (p.stream || !a->dx || p.dw.items() > 256);
+    // otherwise one launch where both use the same tile, the longer tiles first
+    const bool together = a->dx && a->dw && !p.stream && !short_dw && p.dx.tile == p.dw.tile;
     both.queue = prep.queues + kGemmXcds;
     if (a->dx && p.stream) {
       LossStream s{};
@@ -466,7 +470,10 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       both.count = together ? 2 : 1;
       LOSS_TRY(launch_loss_gemm(both, kLossOut, p.dx.tile, st), "dx launch");
     }
-    if (a->dw && !together) {
+    if (a->dw && short_dw) {
+      mw.tn = int(p.hp / 256);
+      LOSS_TRY(launch_loss_dw(mw, rows <= 32 ? 1 : rows <= 64 ? 2 : 4, st), "dw launch");
+    } else if (a->dw && !together) {
       both.g[0] = mw;
       both.count = 1;
       both.queue = prep.queues + 2 * kGemmXcds;

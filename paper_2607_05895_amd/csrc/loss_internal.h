@@ -67,8 +67,9 @@ struct LossGemm2 {
 };
 
 // Products for a few tokens (at most 32 MI), where reading w counts: w is read as it lies, once, with no packed copy.
-//   logits: tiles of 256 ids, K = h in steps of 64;  dx: tiles of 256 columns of h, K = v in steps of 64, cut into `splits` ranges of
-//   kper steps, whose fp32 results lie row-major (32 MI x ldo) one after another in part.
+//   logits: tiles of stream_rows(MI) ids, K = h in steps of 16384 / stream_rows;  dx: tiles of 256 columns of h, K = v in steps of
+//   64, cut into `splits` ranges of kper steps, whose fp32 results lie row-major (32 MI x ldo) one after another in part.
+__host__ __device__ constexpr int stream_rows(int mi) { return mi <= 2 ? 128 : 256; }
 struct LossStream {
   const uint16_t *P, *w;     // P: x, or dz; panel blocked with ldp columns
   int64_t ldp, v, h;
@@ -178,6 +179,8 @@ struct LossJoin {
 
 enum { kLossLogits = 0, kLossOut = 1 };
 hipError_t launch_loss_gemm(const LossGemm2& a, int kind, int tile, hipStream_t st);
+// dw of `steps` (1, 2 or 4) times 32 tokens at most, bf16
+hipError_t launch_loss_dw(const LossGemm& a, int steps, hipStream_t st);
 hipError_t launch_loss_stream(const LossStream& a, int mi, int kind, hipStream_t st);
 hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st);
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st);
