@@ -511,7 +511,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         const float ones = half_sum(__builtin_rintf(all - s));
         s = half_sum(s);
         if (left > 0 && eh == 0) {
-          const int64_t at = int64_t(c0 >> 6) * a.ldr + row;
+          const int64_t at = int64_t(c0 >> 6) * a.gstep + row * a.rstep;
           a.gm[at] = m * a.inv_t;
           a.gs[at] = s + (ones - 1.0f);
         }
@@ -854,11 +854,13 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
   m = hi;
 }
 
-// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB, BATCH at a time.
+// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB. Many tokens: 32 rows,
+// whose partials of a group lie together. Few: one row, whose partials lie in one piece (128256 ids, 48 tokens: 7 us; with four
+// rows each and the other layout 19.5, when a workgroup reads four times the bytes it needs).
 template <int RPB>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
-  constexpr int GS = 1024 / RPB, BATCH = RPB == 4 ? 16 : 8;
-  __shared__ float sm[GS][RPB + 1], ss[GS][RPB + 1];
+  constexpr int GS = 1024 / RPB, BATCH = 8;
+  __shared__ float sm[16][RPB + 1], ss[16][RPB + 1];
   __shared__ double part[16];
   const int blocks = a.rows_pad / RPB;
   if (int(blockIdx.x) == blocks) {  // (the extra workgroup)
@@ -872,28 +874,46 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
     // (asked for here, needed at the end)
     const bool mine = gl == 0 && r < a.rows;
     const float on = mine ? a.on[r] : 0.0f, ent = mine ? a.ent[r] : 0.0f, wt = mine && a.weight ? a.weight[r] : 1.0f;
-    const float q0 = mine ? a.q[r * a.k] : 0.0f, z0 = mine ? a.zt[r * a.k] : 0.0f;
-    const int id0 = mine ? a.id[r * a.k] : -1;
-    for (int g = gl; g < a.groups; g += BATCH * GS) {
+    for (int g = gl; g < (r < a.rows ? a.groups : 0); g += BATCH * GS) {
       float gm[BATCH], gs[BATCH];
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) {
         const bool in = g + i * GS < a.groups;
-        gm[i] = in ? a.gm[(g + i * GS) * a.ldr + r] : none;
-        gs[i] = in ? a.gs[(g + i * GS) * a.ldr + r] : 0.0f;
+        const int64_t at = (g + i * GS) * a.gstep + r * a.rstep;
+        gm[i] = in ? a.gm[at] : none;
+        gs[i] = in ? a.gs[at] : 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < BATCH; ++i) join_softmax(m, s, gm[i], gs[i]);
     }
-    sm[gl][rl] = m;
-    ss[gl][rl] = s;
+    // the lanes of a row, then the waves
 #pragma unroll
-    for (int o = GS / 2; o > 0; o >>= 1) {
+    for (int o = 32; o >= RPB; o >>= 1) join_softmax(m, s, __shfl_xor(m, o), __shfl_xor(s, o));
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) < RPB) {
+      sm[w][rl] = m;
+      ss[w][rl] = s;
+    }
+    __syncthreads();
+    if (gl == 0) {
+      for (int i = 1; i < 16; ++i) join_softmax(m, s, sm[i][rl], ss[i][rl]);
+      sm[0][rl] = m;
+    }
+    __syncthreads();
+    // sum of q (m - z) over the row's targets
+    const float top = sm[0][rl];
+    float d = 0.0f;
+    for (int j = gl; j < (r < a.rows ? a.k : 0); j += GS) {
+      const float q = a.q[r * a.k + j], z = a.zt[r * a.k + j];
+      if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (top - z);
+    }
+#pragma unroll
+    for (int o = 32; o >= RPB; o >>= 1) d += __shfl_xor(d, o);
+    if (a.k > 64 / RPB) {  // (more than one wave's)
+      if ((threadIdx.x & 63) < RPB) ss[w][rl] = d;
       __syncthreads();
-      if (gl < o) {
-        join_softmax(m, s, sm[gl + o][rl], ss[gl + o][rl]);
-        sm[gl][rl] = m;
-        ss[gl][rl] = s;
+      if (gl == 0) {
+        for (int i = 1; i < 16; ++i) d += ss[i][rl];
       }
     }
     if (gl == 0) {
@@ -903,12 +923,7 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
         const float ls = log1pf(s), lse = m + ls;
         float loss = 0.0f;
         if (on != 0.0f) {
-          float d = ent + (q0 > 0.0f && id0 >= 0 ? q0 * (m - z0) : 0.0f);
-          for (int j = 1; j < a.k; ++j) {
-            const float q = a.q[r * a.k + j];
-            if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (m - a.zt[r * a.k + j]);
-          }
-          loss = (d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
+          loss = (ent + d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
         }
         a.row[r] = float4{m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
         if (a.token_loss) a.token_loss[r] = loss;
@@ -934,7 +949,7 @@ __global__ __launch_bounds__(1024) void loss_total_kernel(const LossTotal a) {
 // then out. Bound by HBM: 2 bytes read and 2 written per logit (bf16).
 template <bool F32>
 __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
-  // chunk c of 8 columns of row r at r * 32 + (c ^ r) (fp32: two 16-byte halves, 32 chunks apart per row pair)
+  // 16-byte chunk c of row r in slot c ^ r
   __shared__ __attribute__((aligned(16))) uint8_t smem[32 * 256 * (F32 ? 4 : 2)];
   const int tc = a.v_pad / 256;
   if (int64_t(blockIdx.x) == int64_t(a.rows_pad / 32) * tc) {  // (one more workgroup, for the loss)
@@ -965,7 +980,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
       *(lptr<f32x4_t>)(smem + at32(r, cl + 4)) = f32x4_t{x[4], x[5], x[6], x[7]};
     } else {
       const u32x4 v = *(gptr<const u32x4>)(a.codes + blk_index(row, c, a.ldc));
-      const float m = c < a.v ? a.gm[(c >> a.group_shift) * a.ldr + row] : 0.0f;
+      const float m = c < a.v ? a.gm[(c >> a.group_shift) * a.gstep + row * a.rstep] : 0.0f;
       const float base = (m - rw.x) * kLog2e;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -978,21 +993,29 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
     }
   }
   __syncthreads();
-  for (int i = t; i < 32 * a.k; i += 256) {
+  auto target = [&](int i, int id) {
+    id -= int(c0);
+    if (id < 0 || id >= 256) return;
     const int r = i / a.k;
-    const int64_t row = r0 + r, at = row * a.k + (i - r * a.k);
-    const int id = a.id[at] - int(c0);
-    if (id < 0 || id >= 256 || a.id[at] < 0) continue;
+    const int64_t row = r0 + r;
     const float4 rw = a.row[row];
-    if (rw.z == 0.0f) continue;
+    if (rw.z == 0.0f) return;
     float q = 0.0f;  // of all slots with this id: each of them writes the same value
-    for (int j = 0; j < a.k; ++j) q += a.id[row * a.k + j] == a.id[at] ? a.q[row * a.k + j] : 0.0f;
-    const float d = a.zt[at] - rw.x, e = expf(d);
+    for (int j = 0; j < a.k; ++j) q += a.id[row * a.k + j] == id + int(c0) ? a.q[row * a.k + j] : 0.0f;
+    const float d = a.zt[r0 * a.k + i] - rw.x, e = expf(d);
     // p - q, from what is exact where both are near 1
     const float pq = e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * rw.y : e - q * (1.0f + rw.y);
     const float x = rw.z * (pq + rw.w * e) / (1.0f + rw.y);
     if constexpr (F32) *(lptr<float>)(smem + at32(r, id)) = x;
     else *(lptr<uint16_t>)(smem + at16(r, id)) = uint16_t(pack_bf16x2(x, 0.0f));
+  };
+  for (int i = t; i < 32 * a.k; i += 8 * 256) {  // eight ids asked for at a time
+    int id[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) id[e] = i + e * 256 < 32 * a.k ? a.id[r0 * a.k + i + e * 256] : -1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (id[e] >= 0) target(i + e * 256, id[e]);
   }
   __syncthreads();
 #pragma unroll
@@ -1213,7 +1236,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
           const float ones = half_sum(__builtin_rintf(all - s));
           s = half_sum(s);
           if (fh == 0) {
-            const int64_t at = int64_t(c0 >> 5) * a.ldr + row;
+            const int64_t at = int64_t(c0 >> 5) * a.gstep + row * a.rstep;
             a.gm[at] = m * a.inv_t;
             a.gs[at] = s + (ones - 1.0f);
           }
@@ -1416,9 +1439,9 @@ hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st) {
 }
 
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st) {
-  const int per = loss_rows_per_block(a.rows_pad);
+  const int per = a.gstep == 1 ? 1 : 32;
   const dim3 grid(unsigned(a.rows_pad / per + (a.denom ? 1 : 0)));
-  if (per == 4) hipLaunchKernelGGL(loss_rows_kernel<4>, grid, dim3(1024), 0, st, a);
+  if (per == 1) hipLaunchKernelGGL(loss_rows_kernel<1>, grid, dim3(1024), 0, st, a);
   else hipLaunchKernelGGL(loss_rows_kernel<32>, grid, dim3(1024), 0, st, a);
   return hipGetLastError();
 }

@@ -56,6 +56,7 @@ struct Plan {
   int64_t n = 0, v = 0, h = 0, k = 1;
   int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0, ldw = 0;
   int group = kLossGroup;       // columns of a softmax partial
+  int64_t gstep = 0, rstep = 0; // elements from a group's, from a row's partial to the next one
   Gemm logits, dx, dw;
   // offsets
   size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, queues = 0, row = 0, zt = 0, gm = 0, gs = 0;
@@ -175,6 +176,9 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
     p.chunk = std::min(p.n_pad, most);
   }
   const int64_t vsteps = up(p.v, 32) / 32, groups = (p.vp + p.group - 1) / p.group;
+  // many tokens: the logits' lanes (rows) store whole lines; few: a row's partials are read in one piece
+  p.gstep = p.chunk > 256 ? p.chunk : 1;
+  p.rstep = p.chunk > 256 ? 1 : groups;
   size_t part = 0;
   if (p.stream) {
     if (a->dx) {
@@ -335,7 +339,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       z.inv_t = inv_t;
       z.gm = f32p(p.gm);
       z.gs = f32p(p.gs);
-      z.ldr = p.chunk;
+      z.gstep = p.gstep;
+      z.rstep = p.rstep;
       z.ids = ids;
       z.zt = f32p(p.zt);
       z.k = int32_t(k);
@@ -354,7 +359,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       z.inv_t = inv_t;
       z.gm = f32p(p.gm);
       z.gs = f32p(p.gs);
-      z.ldr = p.chunk;
+      z.gstep = p.gstep;
+      z.rstep = p.rstep;
       z.ids = ids;
       z.zt = f32p(p.zt);
       z.k = int32_t(k);
@@ -367,7 +373,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     LossRows rw{};
     rw.gm = f32p(p.gm);
     rw.gs = f32p(p.gs);
-    rw.ldr = p.chunk;
+    rw.gstep = p.gstep;
+    rw.rstep = p.rstep;
     rw.groups = int((p.v + p.group - 1) / p.group);
     rw.rows = int(rows);
     rw.rows_pad = int(rows_pad);
@@ -401,7 +408,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     gr.dz = u16p(p.codes);
     gr.dz_part = dzpart;
     gr.gm = rw.gm;
-    gr.ldr = p.chunk;
+    gr.gstep = p.gstep;
+    gr.rstep = p.rstep;
     gr.row = rw.row;
     gr.id = ids;
     gr.q = q;

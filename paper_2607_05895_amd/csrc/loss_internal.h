@@ -41,8 +41,8 @@ struct LossGemm {
   int32_t op;                                      // kLossDx, kLossDw (gradients)
   // logits: softmax partials per row and 64 columns, the targets' logits, and the logits themselves (or none of them)
   float inv_t;
-  float *gm, *gs;                                  // [group][ldr]: largest logit; sum of the others' exp relative to it
-  int64_t ldr;
+  float *gm, *gs;                                  // (group, row): largest logit; sum of the others' exp relative to it
+  int64_t gstep, rstep;                            // elements from a group, from a row to the next
   const int32_t* ids;                              // rows x k columns (negative: none)
   float* zt;                                       // rows x k logits of those
   int32_t k;
@@ -75,8 +75,8 @@ struct LossStream {
   int64_t ldp, v, h;
   int32_t nk, tiles, splits, kper;
   float inv_t;
-  float *gm, *gs;            // per row and 32 columns, [group][ldr]
-  int64_t ldr;
+  float *gm, *gs;            // per row and 32 columns
+  int64_t gstep, rstep;
   const int32_t* ids;
   float* zt;
   int32_t k;
@@ -133,7 +133,7 @@ struct LossTotal {
 // count).
 struct LossRows {
   const float *gm, *gs;
-  int64_t ldr;
+  int64_t gstep, rstep;        // (gstep 1: one row per workgroup)
   int32_t groups, rows, rows_pad, k;
   const int32_t* id;
   const float *q, *ent, *on, *weight, *zt;
@@ -156,7 +156,7 @@ struct LossGrad {
   uint16_t* dz;                // (codes: dz = codes)
   int64_t dz_part;
   const float* gm;
-  int64_t ldr;
+  int64_t gstep, rstep;
   const float4* row;
   const int32_t* id;
   const float *q, *zt;
@@ -189,7 +189,5 @@ hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st);
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st);
 hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st);
 hipError_t launch_scale_grad(void* p, int64_t n, int bf16, const float* factor, hipStream_t st);
-// Rows of one workgroup of the rows launch.
-constexpr int loss_rows_per_block(int rows_pad) { return rows_pad <= 256 ? 4 : 32; }
 
 }  // namespace mfsdp
