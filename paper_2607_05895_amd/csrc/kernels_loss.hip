@@ -734,15 +734,40 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
     s += e[i];
   }
   s = wave_sum(s);
-  float ent = 0.0f;
+  float ent = 0.0f, q[PER], sum[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    sum[i] = q[i] = on ? e[i] / s : 0.0f;
+    if (q[i] > 0.0f) ent += q[i] * ((lg[i] - m) - logf(s));
+  }
+  // an id given more than once: its first slot takes the weights of all, the others become empty
+  if (l.k > 1) {
+    bool again[PER] = {};
+#pragma unroll
+    for (int b = 0; b < PER; ++b)
+      for (int x = 0; x < min(64, l.k - b * 64); ++x) {
+        const int idx = __builtin_amdgcn_readlane(id[b], x), jx = b * 64 + x;
+        const float qx = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(q[b]), x));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const bool same = id[i] == idx;
+          again[i] |= same && jx < i * 64 + ln;
+          sum[i] += same && jx > i * 64 + ln ? qx : 0.0f;
+        }
+      }
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (again[i]) {
+        id[i] = -1;
+        sum[i] = 0.0f;
+      }
+  }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int j = i * 64 + ln;
-    const float q = on ? e[i] / s : 0.0f;
-    if (q > 0.0f) ent += q * ((lg[i] - m) - logf(s));
     if (j < l.k) {
       a.id[r * l.k + j] = on ? id[i] : -1;
-      a.q[r * l.k + j] = q;
+      a.q[r * l.k + j] = sum[i];
     }
   }
   ent = wave_sum(ent);
@@ -1000,9 +1025,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
     const int64_t row = r0 + r;
     const float4 rw = a.row[row];
     if (rw.z == 0.0f) return;
-    float q = 0.0f;  // of all slots with this id: each of them writes the same value
-    for (int j = 0; j < a.k; ++j) q += a.id[row * a.k + j] == id + int(c0) ? a.q[row * a.k + j] : 0.0f;
-    const float d = a.zt[r0 * a.k + i] - rw.x, e = expf(d);
+    const float q = a.q[r0 * a.k + i], d = a.zt[r0 * a.k + i] - rw.x, e = expf(d);
     // p - q, from what is exact where both are near 1
     const float pq = e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * rw.y : e - q * (1.0f + rw.y);
     const float x = rw.z * (pq + rw.w * e) / (1.0f + rw.y);
