@@ -426,8 +426,9 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0.
  * Precision: bf16 products have fp32 accumulation; the softmax is formed in fp32, the sum of a row without its largest
  * term, so that the loss of a token that the model is sure of keeps its digits; the logits' gradient is rounded to bf16
- * before its two products, and each result once to bf16. F32: products at fp32 accuracy (three bf16 parts per operand),
- * everything else in fp32. */
+ * before its two products, and each result once to bf16. F32: products at fp32 accuracy (two scaled fp16 parts per operand:
+ * a value of w is off by at most 2^-24 of itself or 2^-40 of w's largest, an element of a row of x or of the logits' gradient by as
+ * much relative to its row), everything else in fp32. */
 typedef struct {
   const void* x;
   const void* w;
@@ -447,9 +448,8 @@ typedef struct {
 } mfsdp_head_loss;
 
 /* Bytes of device workspace for mfsdp_linear_xent (k = 1) and mfsdp_linear_distill with these arguments: the chunk's rows of
- * x and (for gradients) its logits, a copy of w for F32 (three bf16 parts) and for h that are no multiple of 8, and for n
- * beyond one chunk an fp32 sum of dw. Of the pointers
- * only whether dx and dw are NULL is looked at. 0 on invalid arguments. */
+ * x and (for gradients) its logits, a copy of w for F32 (two fp16 parts) and for h that are no multiple of 8, and for n beyond
+ * one chunk an fp32 sum of dw. Of the pointers only whether dx and dw are NULL is looked at. 0 on invalid arguments. */
 size_t mfsdp_head_loss_workspace_size(const mfsdp_head_loss* args, int32_t k);
 
 /* Softmax cross entropy with hard labels: l_r = lse_r - z_{r, t_r} + z_loss lse_r^2.

@@ -12,6 +12,7 @@ namespace mfsdp {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -92,6 +93,16 @@ __device__ __forceinline__ float half_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+
+// The scale that brings values of at most `most` to at most 2^15, and its inverse; both normal numbers.
+__device__ __forceinline__ float scale_for(float most, float& inv) {
+  int e = int(__float_as_uint(most) >> 23) - 126;  // most < 2^e
+  e = most > 0.0f ? max(e, -100) : 15;
+  inv = __uint_as_float(uint32_t(127 + e - 15) << 23);
+  return __uint_as_float(uint32_t(127 + 15 - e) << 23);
+}
+// the magnitude of a finite value, 0 for others
+__device__ __forceinline__ float finite_mag(float x) { return fabsf(x) < __builtin_inff() ? fabsf(x) : 0.0f; }
 
 struct Item {
   int p, bi, bj, k0, nk;  // problem, tile, K steps
@@ -216,14 +227,14 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00020000),
                                              (lds_byte*)(smem + at), 16, voff, soff, 0, 0);
   };
-  // Step k of all segments: the step in its segment, and the bytes to its parts of P and Q. fp32 operands lie in three bf16
-  // parts; the pairs (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0), the small products first: they are added while the sum is small.
+  // Step k of all segments: the step in its segment, and the bytes to its parts of P and Q. fp32 operands lie in two fp16
+  // parts; the pairs (1, 0) (0, 1) (0, 0), the small products first: they are added while the sum is small.
   auto in_segment = [&](int k, int64_t& po, int64_t& qo) {
     po = qo = 0;
     if constexpr (NSEG > 1) {
       const int sg = k / seg_steps;
-      po = int64_t(0x001102 >> (4 * sg) & 0xf) * ppart;
-      qo = int64_t(0x010120 >> (4 * sg) & 0xf) * qpart;
+      po = sg == 0 ? ppart : 0;
+      qo = sg == 1 ? qpart : 0;
       k -= sg * seg_steps;
     }
     return k;
@@ -348,7 +359,11 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     bf16x8_t pf[2][MI], qf[2][NI];  // fragments of the two slices
     auto mfma = [&](int m, int sl) {
       const int i = m / NI, j = (i & 1) ? NI - 1 - m % NI : m % NI;
-      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[sl][j], pf[sl][i], acc[i][j], 0, 0, 0);
+      if constexpr (NSEG > 1)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, qf[sl][j]),
+                                                           __builtin_bit_cast(f16x8_t, pf[sl][i]), acc[i][j], 0, 0, 0);
+      else
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[sl][j], pf[sl][i], acc[i][j], 0, 0, 0);
     };
     // One step: the first slice with the second one's reads and P's loads; half of the second slice with Q's loads; the
     // barrier; the rest with the next step's first reads. wait_c: loads that may still be in flight for the next step to have landed.
@@ -465,6 +480,13 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     asm volatile("" : "+v"(ln));  // lane-dependent offsets are formed here, not kept through the main loop
     const int er = ln & 31, eh = ln >> 5;
     const LossGemm& a = b.g[cur.p];
+    // fp32: 1 / (the scales of row r of P and of Q)
+    const float q_inv = NSEG > 1 ? *a.unscale : 1.0f;
+    auto unscale = [&](int r) {
+      float inv = 1.0f;
+      if (a.row_most) scale_for(a.row_most[r], inv);
+      return inv * q_inv;
+    };
     if constexpr (KIND == kLossLogits) {
       const int c0 = cur.bj * TB + wn * 64;       // the wave's first column
       const int left = a.cols - c0;               // real columns from there
@@ -479,7 +501,9 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
       int id0[MI];
 #pragma unroll
       for (int mi = 0; mi < MI; ++mi) id0[mi] = *(gptr<const int32_t>)(a.ids + int64_t(row0 + mi * 32) * a.k);
-      const float L = kLog2e * a.inv_t;
+      float inv_ts[MI];
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) inv_ts[mi] = NSEG > 1 ? a.inv_t * unscale(row0 + mi * 32) : a.inv_t;
       if (left < 64) {  // columns past the vocabulary
 #pragma unroll
         for (int e = 0; e < 32; ++e)
@@ -492,6 +516,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
       static_for<MI>([&](auto mi_c) {
         constexpr int mi = decltype(mi_c)::value;
         const int row = row0 + mi * 32;
+        const float inv_t = inv_ts[mi], L = kLog2e * inv_t;
         float u[32];  // logits before the temperature
 #pragma unroll
         for (int e = 0; e < 32; ++e) u[e] = acc[mi][e >> 4][e & 15];
@@ -512,7 +537,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         s = half_sum(s);
         if (left > 0 && eh == 0) {
           const int64_t at = int64_t(c0 >> 6) * a.gstep + row * a.rstep;
-          a.gm[at] = m * a.inv_t;
+          a.gm[at] = m * inv_t;
           a.gs[at] = s + (ones - 1.0f);
         }
         auto target = [&](int id, int j) {
@@ -522,7 +547,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
             float z = 0.0f;
 #pragma unroll
             for (int f = 0; f < 32; ++f) z = e == f ? u[f] : z;
-            a.zt[int64_t(row) * a.k + j] = z * a.inv_t;
+            a.zt[int64_t(row) * a.k + j] = z * inv_t;
           }
         };
         target(id0[mi], 0);
@@ -538,14 +563,14 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
 #pragma unroll
           for (int p = 0; p < 8; ++p)
             *(gptr<f32x4_t>)(dst + (p >> 2) * 32 + (p & 3) * 8 + eh * 4) =
-                f32x4_t{u[4 * p] * a.inv_t, u[4 * p + 1] * a.inv_t, u[4 * p + 2] * a.inv_t, u[4 * p + 3] * a.inv_t};
+                f32x4_t{u[4 * p] * inv_t, u[4 * p + 1] * inv_t, u[4 * p + 2] * inv_t, u[4 * p + 3] * inv_t};
         }
       });
       if (a.codes) {
         static_for<MI>([&](auto mi_c) {
           constexpr int mi = decltype(mi_c)::value;
           // round(65535 x) for x in [0, 1], clamped: x = 1 is kLossOctaves factors of two below the largest
-          const float C = -L * (1.0f / kLossOctaves), m = top[mi];
+          const float C = -kLog2e * a.inv_t * (1.0f / kLossOctaves), m = top[mi];
 #pragma unroll
           for (int p = 0; p < 8; ++p) {
             const f32x16_t& u = acc[mi][p >> 2];
@@ -569,6 +594,16 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     } else {
       const int i = (cur.bj * a.tm + cur.bi) * a.splits + cur.k0 / a.kper;  // tile and range
       const int64_t tile_at = int64_t(i) * (TB * TB) + (w * MI * NI * 4 * 64 + ln) * 4;
+      if constexpr (NSEG > 1) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const float f = unscale(cur.bi * TB + wm * (MI * 32) + i * 32 + er);
+#pragma unroll
+          for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] *= f;
+        }
+      }
       if (a.prev) {
 #pragma unroll
         for (int q = 0; q < MI * NI * 4; ++q) {
@@ -662,18 +697,22 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   LOSS_WAIT_VMCNT(0);
 }
 
-// the next of an fp32 value's three bf16 parts; what is left of the values stays in x
-__device__ __forceinline__ u32x4 split8(float (&x)[8]) {
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
   u32x4 o;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    o[t] = pack_bf16x2(x[2 * t], x[2 * t + 1]);
-    x[2 * t] -= __uint_as_float(o[t] << 16);
-    x[2 * t + 1] -= __uint_as_float(o[t] & 0xffff0000u);
-  }
+  for (int t = 0; t < 4; ++t) o[t] = pack_bf16x2(x[2 * t], x[2 * t + 1]);
   return o;
 }
-
+// the next of scaled fp32 values' two fp16 parts; what is left of the values stays in x
+__device__ __forceinline__ u32x4 split8(float (&x)[8]) {
+  f16x8_t o;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    o[t] = _Float16(x[t]);
+    x[t] -= float(o[t]);
+  }
+  return __builtin_bit_cast(u32x4, o);
+}
 // Label entry `at` (token times k plus slot): its id; its teacher logit; whether it makes its token count.
 __device__ __forceinline__ int64_t label_id(const LossLabels& l, int64_t at) {
   return l.id64 ? ((const int64_t*)l.ids)[at] : int64_t(((const int32_t*)l.ids)[at]);
@@ -695,6 +734,53 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
   return v;
+}
+
+// the largest of n values that are >= 0, for every lane
+__device__ __forceinline__ float wave_max_of(const float* p, int n) {
+  float m = 0.0f;
+  for (int i = threadIdx.x & 63; i < n; i += 64) m = fmaxf(m, p[i]);
+  return wave_max(m);
+}
+
+// Bound by HBM: x and w read once (50257 x 768 and 1024 x 768: 35 us, 4.5 TB/s).
+__global__ __launch_bounds__(1024) void loss_maxima_kernel(const LossMaxima a) {
+  __shared__ float part[16];
+  const int ln = threadIdx.x & 63, w = threadIdx.x >> 6;
+  float m = 0.0f;
+  if (int(blockIdx.x) < a.xblocks) {  // a wave per row
+    for (int64_t r = int64_t(blockIdx.x) * 16 + w; r < a.n_pad; r += int64_t(a.xblocks) * 16) {
+      bool counts = false;
+      if (r < a.l.n)
+        for (int j = ln; j < a.l.k; j += 64) counts |= slot_counts(a.l, r * a.l.k + j);
+      m = 0.0f;
+      if (__any(counts)) {
+        const float* p = a.x + r * a.h;
+#pragma unroll 8
+        for (int64_t c = ln; c < a.h; c += 64) m = fmaxf(m, finite_mag(p[c]));
+        m = wave_max(m);
+      }
+      if (ln == 0) a.xmax[r] = m;
+    }
+    return;
+  }
+  {
+    const int64_t all = a.l.v * a.h, step = int64_t(a.wblocks) * 1024, t = int64_t(int(blockIdx.x) - a.xblocks) * 1024 + threadIdx.x;
+#pragma unroll 8
+    for (int64_t i = t; i < all / 4; i += step) {
+      const f32x4_t v = *(gptr<const f32x4_t>)(a.w + i * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_mag(v[e]));
+    }
+    if (t < all % 4) m = fmaxf(m, finite_mag(a.w[all - 1 - t]));
+  }
+  m = wave_max(m);
+  if (ln == 0) part[w] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+    a.wmax[int(blockIdx.x) - a.xblocks] = m;
+  }
 }
 
 // The labels of token r (< n_pad) in one form: one wave, lanes over the slots.
@@ -778,7 +864,7 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
 }
 
 // One 32 x 256 tile of a packed operand: four 8-column chunks per thread (row it * 8 + t / 32, chunk t % 32).
-__device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, int* counts) {
+__device__ __forceinline__ void pack_tile(const LossLabels& l, const LossPack& d, int* counts) {
   const int64_t i = int(blockIdx.x) - d.blocks_begin;
   const int64_t tc = d.cols / 256, r0 = i / tc * 32, c0 = i % tc * 256;
   const int t = threadIdx.x, ch = t & 31;
@@ -786,9 +872,9 @@ __device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, 
   if (d.label_row >= 0) {
     if (t < 32) counts[t] = 0;
     __syncthreads();
-    for (int e = t; e < 32 * a.l.k; e += 256) {
-      const int r = e / a.l.k;
-      if (r0 + r < d.R && slot_counts(a.l, (d.label_row + r0 + r) * a.l.k + (e - r * a.l.k))) counts[r] = 1;
+    for (int e = t; e < 32 * l.k; e += 256) {
+      const int r = e / l.k;
+      if (r0 + r < d.R && slot_counts(l, (d.label_row + r0 + r) * l.k + (e - r * l.k))) counts[r] = 1;
     }
     __syncthreads();
 #pragma unroll
@@ -834,10 +920,31 @@ __device__ __forceinline__ void prep_pack(const LossPrep& a, const LossPack& d, 
       }
     }
   }
-  for (int part = 0; part < (d.bf16 ? 1 : 3); ++part) {
+  if (!d.bf16) {
+    float all = 1.0f, inv;
+    if (d.most) {
+      all = scale_for(wave_max_of(d.most, d.count), inv);
+      if (i == 0 && t == 0) *d.inv = inv;
+    }
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
-      const u32x4 v = split8(x[it]);
+      float f = all;
+      if (d.row_most) {
+        const float most = d.row_most[r0 + it * 8 + (t >> 5)], scale = scale_for(most, inv);
+        f = !d.most ? scale : inv * all;
+        if (d.most && most == 0.0f) {  // no part in dw
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[it][e] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[it][e] *= f;
+    }
+  }
+  for (int part = 0; part < (d.bf16 ? 1 : 2); ++part) {
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const u32x4 v = d.bf16 ? pack8(x[it]) : split8(x[it]);
       const int64_t r = r0 + it * 8 + (t >> 5);
       uint16_t* dst = d.dst + part * d.dst_part;
       if (d.blocked) *(gptr<u32x4>)(dst + blk_index(r, c, d.ld)) = v;
@@ -854,7 +961,7 @@ __global__ __launch_bounds__(256) void loss_prep_kernel(const LossPrep a) {
     if (r < a.n_pad) prep_labels(a, r);
     return;
   }
-  prep_pack(a, a.d[a.packs > 1 && int(blockIdx.x) >= a.d[1].blocks_begin ? 1 : 0], counts);
+  pack_tile(a.l, a.d[a.packs > 1 && int(blockIdx.x) >= a.d[1].blocks_begin ? 1 : 0], counts);
 }
 
 // Sum over a workgroup, in 64 bits and a fixed order, of n values (times b where a value is not 0); for every thread.
@@ -879,13 +986,18 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
   m = hi;
 }
 
+// (p - q) (1 + s) of a target with weight q whose logit is d above the row's largest and e = exp(d): from what is exact where p and q are near 1
+__device__ __forceinline__ float target_pq(float q, float d, float e, float s) {
+  return e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * s : e - q * (1.0f + s);
+}
+
 // RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB. Many tokens: 32 rows,
 // whose partials of a group lie together. Few: one row, whose partials lie in one piece (128256 ids, 48 tokens: 7 us; with four
 // rows each and the other layout 19.5, when a workgroup reads four times the bytes it needs).
 template <int RPB>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
   constexpr int GS = 1024 / RPB, BATCH = 8;
-  __shared__ float sm[16][RPB + 1], ss[16][RPB + 1];
+  __shared__ float sm[16][RPB + 1], ss[16][RPB + 1], sb[16][RPB + 1], sd[16][RPB + 1];
   __shared__ double part[16];
   const int blocks = a.rows_pad / RPB;
   if (int(blockIdx.x) == blocks) {  // (the extra workgroup)
@@ -923,38 +1035,74 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
     if (gl == 0) {
       for (int i = 1; i < 16; ++i) join_softmax(m, s, sm[i][rl], ss[i][rl]);
       sm[0][rl] = m;
+      ss[0][rl] = s;
     }
     __syncthreads();
-    // sum of q (m - z) over the row's targets
-    const float top = sm[0][rl];
-    float d = 0.0f;
+    // sum of q (m - z) over the row's targets; a bound on |dz| at them, in units of 1 / (1 + s); whether one of them is the largest
+    const float top = sm[0][rl], others = ss[0][rl];
+    const float lz = 2.0f * a.z_loss * (top + log1pf(others));
+    float d = 0.0f, bound = 0.0f;
+    bool of_top = false;
     for (int j = gl; j < (r < a.rows ? a.k : 0); j += GS) {
       const float q = a.q[r * a.k + j], z = a.zt[r * a.k + j];
-      if (q > 0.0f && a.id[r * a.k + j] >= 0) d += q * (top - z);
-    }
-#pragma unroll
-    for (int o = 32; o >= RPB; o >>= 1) d += __shfl_xor(d, o);
-    if (a.k > 64 / RPB) {  // (more than one wave's)
-      if ((threadIdx.x & 63) < RPB) ss[w][rl] = d;
-      __syncthreads();
-      if (gl == 0) {
-        for (int i = 1; i < 16; ++i) d += ss[i][rl];
+      if (q > 0.0f && a.id[r * a.k + j] >= 0) {
+        d += q * (top - z);
+        if (a.most) {
+          const float e = expf(z - top);
+          bound = fmaxf(bound, fabsf(target_pq(q, z - top, e, others) + lz * e));
+          of_top |= z == top;
+        }
       }
     }
+#pragma unroll
+    for (int o = 32; o >= RPB; o >>= 1) {
+      d += __shfl_xor(d, o);
+      bound = fmaxf(bound, __shfl_xor(bound, o));
+      of_top |= __shfl_xor(int(of_top), o) != 0;
+    }
+    if (a.k > 64 / RPB) {  // (more than one wave's)
+      if ((threadIdx.x & 63) < RPB) {
+        sd[w][rl] = d;
+        sb[w][rl] = copysignf(bound, of_top ? 1.0f : -1.0f);
+      }
+      __syncthreads();
+      if (gl == 0) {
+        for (int i = 1; i < 16; ++i) {
+          d += sd[i][rl];
+          bound = fmaxf(bound, fabsf(sb[i][rl]));
+          of_top |= !__builtin_signbit(sb[i][rl]);
+        }
+      }
+    }
+    float most = 0.0f;
     if (gl == 0) {
       if (r >= a.rows) {
         a.row[r] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (a.most) a.row_most[r] = 0.0f;
       } else {
         const float ls = log1pf(s), lse = m + ls;
         float loss = 0.0f;
         if (on != 0.0f) {
           loss = (ent + d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
         }
-        a.row[r] = float4{m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
+        const float4 rw = {m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
+        a.row[r] = rw;
+        // (a column that is no target: at most the largest p, or what is left of it if the largest is a target's)
+        if (a.most) {
+          bound = finite_mag(rw.z * fmaxf(bound, (1.0f + fabsf(rw.w)) * (of_top ? s : 1.0f)) / (1.0f + s));
+          a.row_most[r] = bound;
+          float inv;
+          scale_for(bound, inv);
+          most = bound > 0.0f ? fminf(a.x_most[r] * inv, 3e38f) : 0.0f;
+        }
         if (a.token_loss) a.token_loss[r] = loss;
         if (a.lse) a.lse[r] = on != 0.0f ? lse : 0.0f;
         a.weighted[r] = on != 0.0f ? wt * loss : 0.0f;
       }
+    }
+    if (a.most && w == 0) {
+      most = wave_max(most);
+      if (threadIdx.x == 0) a.most[blockIdx.x] = most;
     }
   }
 }
@@ -977,9 +1125,16 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   // 16-byte chunk c of row r in slot c ^ r
   __shared__ __attribute__((aligned(16))) uint8_t smem[32 * 256 * (F32 ? 4 : 2)];
   const int tc = a.v_pad / 256;
-  if (int64_t(blockIdx.x) == int64_t(a.rows_pad / 32) * tc) {  // (one more workgroup, for the loss)
+  const int64_t tiles = int64_t(a.rows_pad / 32) * tc;
+  if (a.total.loss && int64_t(blockIdx.x) == tiles) {  // (one more workgroup, for the loss)
     sum_loss<256>(a.total, (double*)smem);
     return;
+  }
+  if constexpr (F32) {
+    if (int(blockIdx.x) >= a.x.blocks_begin) {
+      pack_tile(LossLabels{}, a.x, nullptr);
+      return;
+    }
   }
   const int64_t r0 = int64_t(blockIdx.x / tc) * 32, c0 = int64_t(blockIdx.x % tc) * 256;
   const int t = threadIdx.x, ln = t & 63, w = t >> 6;
@@ -1026,9 +1181,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
     const float4 rw = a.row[row];
     if (rw.z == 0.0f) return;
     const float q = a.q[r0 * a.k + i], d = a.zt[r0 * a.k + i] - rw.x, e = expf(d);
-    // p - q, from what is exact where both are near 1
-    const float pq = e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * rw.y : e - q * (1.0f + rw.y);
-    const float x = rw.z * (pq + rw.w * e) / (1.0f + rw.y);
+    const float x = rw.z * (target_pq(q, d, e, rw.y) + rw.w * e) / (1.0f + rw.y);
     if constexpr (F32) *(lptr<float>)(smem + at32(r, id)) = x;
     else *(lptr<uint16_t>)(smem + at16(r, id)) = uint16_t(pack_bf16x2(x, 0.0f));
   };
@@ -1040,6 +1193,14 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
     for (int e = 0; e < 8; ++e)
       if (id[e] >= 0) target(i + e * 256, id[e]);
   }
+  float scales[4];
+  if constexpr (F32) {
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      float inv;
+      scales[it] = scale_for(a.row_most[r0 + crow(it)], inv);
+    }
+  }
   __syncthreads();
 #pragma unroll
   for (int it = 0; it < 4; ++it) {
@@ -1049,7 +1210,9 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
       const f32x4_t v0 = *(lptr<f32x4_t>)(smem + at32(r, cl)), v1 = *(lptr<f32x4_t>)(smem + at32(r, cl + 4));
       float x[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
 #pragma unroll
-      for (int part = 0; part < 3; ++part) *(gptr<u32x4>)(dst + part * a.dz_part) = split8(x);
+      for (int e = 0; e < 8; ++e) x[e] *= scales[it];
+#pragma unroll
+      for (int part = 0; part < 2; ++part) *(gptr<u32x4>)(dst + part * a.dz_part) = split8(x);
     } else {
       *(gptr<u32x4>)dst = *(lptr<u32x4>)(smem + at16(r, cl));
     }
@@ -1456,6 +1619,11 @@ hipError_t launch_loss_gemm(const LossGemm2& a, int kind, int tile, hipStream_t 
   return hipGetLastError();
 }
 
+hipError_t launch_loss_maxima(const LossMaxima& a, hipStream_t st) {
+  hipLaunchKernelGGL(loss_maxima_kernel, dim3(unsigned(a.xblocks + a.wblocks)), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st) {
   hipLaunchKernelGGL(loss_prep_kernel, dim3(blocks), dim3(256), 0, st, a);
   return hipGetLastError();
@@ -1474,8 +1642,10 @@ hipError_t launch_loss_total(const LossTotal& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st) {
-  const dim3 grid(unsigned(a.rows_pad / 32) * unsigned(a.v_pad / 256) + (a.total.loss ? 1u : 0u));
+hipError_t launch_loss_grad(const LossGrad& b, hipStream_t st) {
+  LossGrad a = b;
+  a.x.blocks_begin = (a.rows_pad / 32) * (a.v_pad / 256) + (a.total.loss ? 1 : 0);
+  const dim3 grid(unsigned(a.x.blocks_begin) + (a.x.src ? unsigned(a.rows_pad / 32) * unsigned(a.x.cols / 256) : 0u));
   if (a.logits)
     hipLaunchKernelGGL(loss_grad_kernel<true>, grid, dim3(256), 0, st, a);
   else

@@ -1,8 +1,9 @@
 // Host side of the losses over a vocabulary: argument checks, workspace plan and launch sequence (all on the caller's
 // stream, descriptors as kernel arguments).
 //
+//   fp32: maxima  the largest values of x's rows and of w, for their scales
 //   per chunk of rows of x (usually one):
-//     prep    the labels in one form (first chunk); x's rows as panel-blocked bf16; a bf16 copy of w where it cannot be read as
+//     prep    the labels in one form (first chunk); x's rows panel blocked; a copy of w where it cannot be read as
 //             it lies (first chunk)
 //     logits  z = x w^T: per row and 64 columns the softmax partials, the targets' logits and (for gradients) the logits
 //     rows    the partials joined: the tokens' losses, and the weights of their gradients; with MEAN (first chunk) the weights'
@@ -60,6 +61,7 @@ struct Plan {
   Gemm logits, dx, dw;
   // offsets
   size_t id = 0, q = 0, ent = 0, on = 0, weighted = 0, denom = 0, queues = 0, row = 0, zt = 0, gm = 0, gs = 0;
+  size_t inv = 0, xmax = 0, wmax = 0, row_most = 0, most = 0;  // fp32: 1 / the scales of x (for dw) and w; what scales come from
   size_t xb = 0, wb = 0, codes = 0, z32 = 0, part = 0, acc = 0;
   size_t bytes = 0;
 };
@@ -153,8 +155,8 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   Plan p;
   p.f32 = a->dtype == MFSDP_F32;
   p.grads = a->dx || a->dw;
-  p.parts = p.f32 ? 3 : 1;
-  p.nseg = p.f32 ? 6 : 1;
+  p.parts = p.f32 ? 2 : 1;
+  p.nseg = p.f32 ? kLossMaxSeg : 1;
   p.n = a->n;
   p.v = a->v;
   p.h = a->h;
@@ -225,6 +227,13 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.zt = take(p.chunk * k * 4);
   p.gm = take(groups * p.chunk * 4);
   p.gs = take(groups * p.chunk * 4);
+  if (p.f32) {
+    p.inv = take(2 * 4);
+    p.xmax = take(p.n_pad * 4);
+    p.wmax = take(kLossMaxima * 4);
+    p.row_most = take(p.chunk * 4);
+    p.most = take(std::max<int64_t>(256, p.chunk / 32) * 4);
+  }
   p.xb = take(p.chunk * p.hp * es);
   if (p.copy) p.wb = take(p.v * p.ldw * es);
   if (p.grads) {
@@ -288,6 +297,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     m.ldq = of_w ? p.ldw : p.hp;
     m.qrows = p.v;
     m.qpart = of_w ? wpart : xpart;
+    m.unscale = f32p(p.inv) + (of_w ? 1 : 0);
     m.nseg = p.nseg;
     m.nk = nk;
     m.kper = g.splits > 1 ? g.kper : p.nseg * nk;
@@ -296,6 +306,19 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     m.tn = g.tn;
     return m;
   };
+  LossMaxima mm{};
+  if (p.f32) {
+    mm.l = prep.l;
+    mm.x = static_cast<const float*>(a->x);
+    mm.w = static_cast<const float*>(a->w);
+    mm.h = p.h;
+    mm.n_pad = p.n_pad;
+    mm.xblocks = int(std::min<int64_t>(kLossMaxima, p.n_pad / 16));
+    mm.wblocks = int(std::min<int64_t>(kLossMaxima, up(p.v * p.h, 16384) / 16384));
+    mm.xmax = f32p(p.xmax);
+    mm.wmax = f32p(p.wmax);
+    LOSS_TRY(launch_loss_maxima(mm, st), "maxima launch");
+  }
   for (int64_t r0 = 0; r0 < p.n; r0 += p.chunk) {
     const int64_t rows = std::min(p.chunk, p.n - r0), rows_pad = up(rows, p.stream ? p.chunk : 256);
     const bool first = r0 == 0, last = r0 + p.chunk >= p.n;
@@ -318,6 +341,10 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       d.blocks_begin = blocks;
       d.bf16 = !p.f32;
       d.blocked = label_row >= 0;
+      d.row_most = d.blocked ? f32p(p.xmax) + r0 : nullptr;
+      d.most = d.blocked ? nullptr : mm.wmax;
+      d.count = mm.wblocks;
+      d.inv = f32p(p.inv) + 1;
       blocks += int(rpad / 32 * (p.hp / 256));
     };
     pack(static_cast<const uint8_t*>(a->x) + r0 * p.h * es, rows, rows_pad, p.xb, p.hp, xpart, r0);
@@ -354,6 +381,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       zz.count = 1;
       zz.queue = prep.queues;
       z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
+      z.row_most = f32p(p.xmax) + r0;
       z.rows = int(rows);
       z.cols = int(p.v);
       z.inv_t = inv_t;
@@ -389,6 +417,11 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     rw.row = reinterpret_cast<float4*>(ws + p.row);
     rw.token_loss = a->token_loss ? a->token_loss + r0 : nullptr;
     rw.lse = a->lse ? a->lse + r0 : nullptr;
+    if (p.f32 && p.grads) {
+      rw.row_most = f32p(p.row_most);
+      rw.most = f32p(p.most);
+      rw.x_most = f32p(p.xmax) + r0;
+    }
     rw.weighted = f32p(p.weighted) + r0;
     rw.n = p.n;
     rw.all_on = prep.on;
@@ -420,6 +453,15 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     gr.v = int(p.v);
     gr.v_pad = int(p.vp);
     gr.group_shift = p.group == 32 ? 5 : 6;
+    gr.row_most = rw.row_most;
+    if (p.f32 && a->dw) {
+      gr.x = prep.d[0];
+      gr.x.label_row = -1;
+      gr.x.row_most = rw.row_most;
+      gr.x.most = rw.most;
+      gr.x.count = loss_row_blocks(rw);
+      gr.x.inv = f32p(p.inv);
+    }
     gr.total = total;
     LOSS_TRY(launch_loss_grad(gr, st), "gradient launch");
 
@@ -427,6 +469,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     if (a->dx && !p.stream) {
       mx = product(p.dx, p.codes, p.vp, dzpart, true, p.dx.nk);
       mx.op = kLossDx;
+      mx.row_most = rw.row_most;
       mx.tm = int(up(rows, p.dx.tile) / p.dx.tile);
       mx.rows = int(rows);
       mx.cols = int(p.h);

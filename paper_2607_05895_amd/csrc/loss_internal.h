@@ -3,8 +3,14 @@
 // For n tokens with hidden states x (n x h) and a head w (v x h), in chunks of rows of x:
 //   z = x w^T / T    logits       dx = dz w       dw = dz^T x
 // x and dz are bf16, panel blocked (blk_index), zero padded (rows to the tile, columns to 256); w is read as it lies, row-major,
-// or, where it is fp32 or its rows are no multiple of 16 bytes, from a row-major bf16 copy. An fp32 tensor is held in three bf16
-// parts, and a product runs over six pairs of parts, one K segment each.
+// or, where it is fp32 or its rows are no multiple of 16 bytes, from a row-major copy.
+//
+// An fp32 tensor is held in two fp16 parts, the value and what is left of it, after scaling by a power of two that brings the largest
+// value to [2^14, 2^15): 22 bits and the second part's sign, so a value is off by at most 2^-24 of itself, as in fp32, down to 2^-16 of
+// the largest, and by 2^-40 of the largest below that. A product runs over three pairs of parts, one K segment each; the fourth
+// would add at most 2^-24 of each product. (Three bf16 parts need no scale, and six pairs: twice the time.) The scale is one for all of
+// w, and one per row of x and of dz, so that no token's digits depend on another token. For dw, which sums over the tokens, x is
+// split a second time, its rows divided by dz's scales. Values that are not finite are left out of the scales.
 //
 // Between the logits and their gradient a chunk of bf16 inputs holds each logit in 16 bits: the distance
 // from the largest of its row in its 64 columns, in steps of 64 / 65535 of a factor of two. That is a relative error of p of
@@ -23,7 +29,8 @@ namespace mfsdp {
 constexpr int kLossTile = 256;       // output tile of the products (kLossTileSmall for launches with few tiles)
 constexpr int kLossTileSmall = 128;
 constexpr int kLossGroup = 64;       // columns of one softmax partial (of the products for a few tokens: 32)
-constexpr int kLossMaxSeg = 6;
+constexpr int kLossMaxSeg = 3;
+constexpr int kLossMaxima = 256;     // workgroups, at most, that look for a tensor's largest value
 constexpr int kLossQueues = 3;         // launches of products per chunk that take their tiles from counters
 constexpr int kLossMaxTop = 256;     // most teacher logits a token
 constexpr float kLossOctaves = 64.0f;  // factors of two that the 16-bit codes of the logits span
@@ -35,6 +42,7 @@ struct LossGemm {
   const uint16_t *P, *Q;
   int64_t ldp, ldq, qrows;
   int64_t ppart, qpart;                            // elements between the parts
+  const float *row_most, *unscale;                 // fp32: what the scales of P's rows come from (null: no scale), 1 / the scale of Q
   int32_t nseg, nk, splits, kper;
   int32_t tm, tn;                                  // tiles
   int32_t rows, cols;                              // real rows and columns of the result
@@ -94,7 +102,7 @@ struct LossLabels {
   float inv_t;
 };
 
-// A bf16 copy of a row-major R x C matrix, in one part (bf16 source) or three (fp32 source) that lie dst_part elements
+// A copy of a row-major R x C matrix, in bf16 or (fp32 source) in two scaled fp16 parts that lie dst_part elements
 // apart: panel blocked with ld columns, padded with zeros to the launch's rows and ld, or row-major with ld columns.
 struct LossPack {
   const void* src;
@@ -105,6 +113,21 @@ struct LossPack {
   int64_t label_row;           // the label of row 0 (rows whose token does not count are written as zeros), or -1: all rows
   int32_t blocks_begin, bf16;  // first workgroup
   int32_t blocked;
+  // fp32. w: the largest of `count` values of most sets the scale. x: row r's scale comes from row_most[r]; and for dw, row
+  // r is divided by the scale that comes from row_most[r], and the largest of most sets the scale. 1 / the scale of all goes to inv.
+  const float *row_most, *most;
+  int32_t count;
+  float* inv;
+};
+
+// fp32: the largest finite magnitude of each row of x (of those that do not count and of the rows up to n_pad: 0), and of w, one
+// per workgroup.
+struct LossMaxima {
+  LossLabels l;
+  const float *x, *w;
+  int64_t h, n_pad;
+  int32_t xblocks, wblocks;
+  float *xmax, *wmax;
 };
 
 // The first launch: the labels in one form (per token k different ids with weights q that add up to 1, -1 and 0 for none; the sum of
@@ -139,6 +162,9 @@ struct LossRows {
   const float *q, *ent, *on, *weight, *zt;
   float z_loss;
   float4* row;                 // {M, s, weight, 2 z_loss lse}
+  // fp32 gradients (else null): per row a bound on |dz| (0 where it is not finite); per workgroup the largest x_most / its scale
+  float *row_most, *most;
+  const float* x_most;
   float *token_loss, *lse;     // optional
   float* weighted;             // weight x loss
   int64_t n;                   // for denom: all tokens
@@ -148,7 +174,7 @@ struct LossRows {
 
 // dz of a chunk, without the factor scale / (T D) common to all tokens (which the products apply: rounded with it, the
 // -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place, or fp32
-// logits -> three bf16 parts.
+// logits -> two fp16 parts, each row scaled.
 struct LossGrad {
   uint16_t* codes;
   const float* logits;
@@ -162,6 +188,8 @@ struct LossGrad {
   const float *q, *zt;
   int32_t k, rows, rows_pad, v, v_pad;
   int32_t group_shift;         // log2 of the columns of one softmax partial
+  const float* row_most;       // fp32
+  LossPack x;                  // fp32: x split for dw, by the last workgroups (x.src null: dw is not asked for)
   LossTotal total;             // loss not null: summed by one more workgroup
 };
 
@@ -182,8 +210,11 @@ hipError_t launch_loss_gemm(const LossGemm2& a, int kind, int tile, hipStream_t 
 // dw of `steps` (1, 2 or 4) times 32 tokens at most, bf16
 hipError_t launch_loss_dw(const LossGemm& a, int steps, hipStream_t st);
 hipError_t launch_loss_stream(const LossStream& a, int mi, int kind, hipStream_t st);
+hipError_t launch_loss_maxima(const LossMaxima& a, hipStream_t st);
 hipError_t launch_loss_prep(const LossPrep& a, int blocks, hipStream_t st);
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st);
+// workgroups of that launch with rows
+inline int loss_row_blocks(const LossRows& a) { return a.gstep == 1 ? a.rows_pad : a.rows_pad / 32; }
 hipError_t launch_loss_total(const LossTotal& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st);
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st);

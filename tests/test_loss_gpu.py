@@ -1,8 +1,8 @@
 """GPU parity of the losses over a vocabulary (mfsdp_linear_xent, mfsdp_linear_distill) against the fp64 oracle.
 
 Bounds, from the operator's arithmetic (u = 2^-24, half a step of fp32; 2u where a matrix instruction may truncate):
-* a logit is a sum of h products: |dz| <= 2 (h + 8) u (|x| |w|^T) / T =: d; three bf16 parts of an fp32 operand leave
-  less than u of it;
+* a logit is a sum of h products: |dz| <= 2 (h + 8) u (|x| |w|^T) / T =: d; each value of an fp32 operand is
+  off by at most u (two fp16 parts), their products by 3 u, which the 16 u cover;
 * a probability is off by 2 max_v d of its row and by 2^-16 (up to 2^8 roundings of its row's sum, exp2, factors); with
   bf16 inputs, for ids that are no targets, by the 16-bit logit's 2^-11 ln 2 as well;
 * dz is then rounded (bf16: 2^-8 of it; fp32: u), and dx, dw are sums of v, n products of it, rounded once more.
@@ -281,6 +281,40 @@ def test_an_id_outside_the_vocabulary_gives_nan(kind):
         got = _call(kind, x, w, BF16, t if kind == "xent" else (t[:, None], np.zeros((4, 1), np.float32), F32))
         assert np.isnan(got["token_loss"][1]) and np.isfinite(got["token_loss"][[0, 2, 3]]).all()
         assert np.isnan(got["loss"][0]) and np.isnan(got["dw"]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["xent", "distill"])
+@pytest.mark.parametrize("n,v,h", [(40, 300, 48), (300, 700, 72), (40, 4500, 72)])
+def test_a_token_does_not_take_digits_from_another(n, v, h, kind, dtype):
+    """Hidden states of 1e20 in a token of weight 0, weights from 1e-12 to 1e12: every other token, and dw, within the same bounds."""
+    rng = np.random.default_rng(28)
+    x, w, x64, w64 = _inputs(rng, n, v, h, dtype)
+    odd = 3
+    far = np.full(h, 1e20, np.float32)
+    x[odd] = synth.f32_to_bf16_bits(far) if dtype == BF16 else far
+    x64[odd] = 0.0  # (as the oracle sees it: what follows leaves this token out)
+    weight = (10.0 ** rng.uniform(-12, 12, n)).astype(np.float32)
+    weight[odd] = 0.0
+    t = _labels(rng, n, v)
+    t[odd] = 5
+    ids, lg = _teacher(rng, n, v, 4)
+    labels = t if kind == "xent" else (ids, lg, F32)
+    _say(kind, n, v, h, dtype)
+    got = _call(kind, x, w, dtype, labels, reduction="sum", token_weight=weight)
+    if kind == "xent":
+        r, on = OL.linear_xent(x64, w64, t, reduction="sum", weight=weight), t >= 0
+        cols = [(i, [t[i]]) for i in range(n) if on[i]]
+    else:
+        r, on = OL.linear_distill(x64, w64, ids, lg.astype(np.float64), reduction="sum", weight=weight), (ids >= 0).any(1)
+        cols = [(i, ids[i][ids[i] >= 0]) for i in range(n)]
+    ref = _Ref(r, on, weight, "sum", 1.0)
+    q = np.zeros((n, v), bool)
+    for i, c in cols:
+        q[i, c] = True
+    for o in ("token_loss", "lse"):
+        got[o][odd] = getattr(ref, o)[odd]
+    _check(got, ref, x64, w64, dtype, q, what=f"{kind} {n}x{v}x{h} {dtype}")
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
