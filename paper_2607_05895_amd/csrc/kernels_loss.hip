@@ -125,6 +125,7 @@ template <int NW, int TB, int NSEG, int KIND>
 __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_kernel(const LossGemm2 b) {
   using G = Grid<NW, TB>;
   constexpr int MI = G::MI, NI = G::NI, HALF = G::HALF, STAGE = G::STAGE, DW = G::DW, PL = G::PL, DLOADS = G::DLOADS;
+  constexpr bool F16 = NSEG == kLossMaxSeg;
   constexpr int kSlabAt = (kStages - 1) * STAGE;  // the part of LDS that no tile's first loads touch
   constexpr int kQAt = 4 * HALF;                  // logits: w's pairs of steps behind x's four steps
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * STAGE];
@@ -228,13 +229,13 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
                                              (lds_byte*)(smem + at), 16, voff, soff, 0, 0);
   };
   // Step k of all segments: the step in its segment, and the bytes to its parts of P and Q. fp32 operands lie in two fp16
-  // parts; the pairs (1, 0) (0, 1) (0, 0), the small products first: they are added while the sum is small.
+  // parts (F16), few tokens' dz in two bf16 parts; the pairs (1, 0), (0, 1) (F16), (0, 0): the small products first, while the sum is small.
   auto in_segment = [&](int k, int64_t& po, int64_t& qo) {
     po = qo = 0;
     if constexpr (NSEG > 1) {
       const int sg = k / seg_steps;
       po = sg == 0 ? ppart : 0;
-      qo = sg == 1 ? qpart : 0;
+      qo = F16 && sg == 1 ? qpart : 0;
       k -= sg * seg_steps;
     }
     return k;
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     bf16x8_t pf[2][MI], qf[2][NI];  // fragments of the two slices
     auto mfma = [&](int m, int sl) {
       const int i = m / NI, j = (i & 1) ? NI - 1 - m % NI : m % NI;
-      if constexpr (NSEG > 1)
+      if constexpr (F16)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, qf[sl][j]),
                                                            __builtin_bit_cast(f16x8_t, pf[sl][i]), acc[i][j], 0, 0, 0);
       else
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     const int er = ln & 31, eh = ln >> 5;
     const LossGemm& a = b.g[cur.p];
     // fp32: 1 / (the scales of row r of P and of Q)
-    const float q_inv = NSEG > 1 ? *a.unscale : 1.0f;
+    const float q_inv = F16 ? *a.unscale : 1.0f;
     auto unscale = [&](int r) {
       float inv = 1.0f;
       if (a.row_most) scale_for(a.row_most[r], inv);
@@ -503,7 +504,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
       for (int mi = 0; mi < MI; ++mi) id0[mi] = *(gptr<const int32_t>)(a.ids + int64_t(row0 + mi * 32) * a.k);
       float inv_ts[MI];
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi) inv_ts[mi] = NSEG > 1 ? a.inv_t * unscale(row0 + mi * 32) : a.inv_t;
+      for (int mi = 0; mi < MI; ++mi) inv_ts[mi] = F16 ? a.inv_t * unscale(row0 + mi * 32) : a.inv_t;
       if (left < 64) {  // columns past the vocabulary
 #pragma unroll
         for (int e = 0; e < 32; ++e)
@@ -558,7 +559,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
 #pragma unroll
           for (int i = 0; i < 16; ++i) target(id[i], j + i);
         }
-        if (a.logits) {
+        if (F16 && a.logits) {
           float* dst = a.logits + int64_t(row) * a.ldc + c0;
 #pragma unroll
           for (int p = 0; p < 8; ++p)
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
                 f32x4_t{u[4 * p] * inv_t, u[4 * p + 1] * inv_t, u[4 * p + 2] * inv_t, u[4 * p + 3] * inv_t};
         }
       });
-      if (a.codes) {
+      if (!F16 && a.codes) {
         static_for<MI>([&](auto mi_c) {
           constexpr int mi = decltype(mi_c)::value;
           // round(65535 x) for x in [0, 1], clamped: x = 1 is kLossOctaves factors of two below the largest
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     } else {
       const int i = (cur.bj * a.tm + cur.bi) * a.splits + cur.k0 / a.kper;  // tile and range
       const int64_t tile_at = int64_t(i) * (TB * TB) + (w * MI * NI * 4 * 64 + ln) * 4;
-      if constexpr (NSEG > 1) {
+      if constexpr (F16) {
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
           const float f = unscale(cur.bi * TB + wm * (MI * 32) + i * 32 + er);
@@ -703,7 +704,16 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
   for (int t = 0; t < 4; ++t) o[t] = pack_bf16x2(x[2 * t], x[2 * t + 1]);
   return o;
 }
-// the next of scaled fp32 values' two fp16 parts; what is left of the values stays in x
+// the next of two bf16 parts, of scaled fp32 values' two fp16 parts; what is left of the values stays in x
+__device__ __forceinline__ u32x4 split8_bf16(float (&x)[8]) {
+  const u32x4 o = pack8(x);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    x[2 * t] -= __uint_as_float(o[t] << 16);
+    x[2 * t + 1] -= __uint_as_float(o[t] & 0xffff0000u);
+  }
+  return o;
+}
 __device__ __forceinline__ u32x4 split8(float (&x)[8]) {
   f16x8_t o;
 #pragma unroll
@@ -1120,10 +1130,11 @@ __global__ __launch_bounds__(1024) void loss_total_kernel(const LossTotal a) {
 
 // One 32 x 256 tile of dz per workgroup of 256: from the logits to LDS, the targets' elements there from their fp32 logits,
 // then out. Bound by HBM: 2 bytes read and 2 written per logit (bf16).
-template <bool F32>
+template <bool F32, int PARTS>
 __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
+  constexpr bool WIDE = PARTS > 1;  // (dz in fp32 in LDS)
   // 16-byte chunk c of row r in slot c ^ r
-  __shared__ __attribute__((aligned(16))) uint8_t smem[32 * 256 * (F32 ? 4 : 2)];
+  __shared__ __attribute__((aligned(16))) uint8_t smem[32 * 256 * (WIDE ? 4 : 2)];
   const int tc = a.v_pad / 256;
   const int64_t tiles = int64_t(a.rows_pad / 32) * tc;
   if (a.total.loss && int64_t(blockIdx.x) == tiles) {  // (one more workgroup, for the loss)
@@ -1156,8 +1167,6 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         x[e] = rw.z != 0.0f && c + e < a.v ? expf((e < 4 ? v0[e & 3] : v1[e & 3]) - rw.x) * f : 0.0f;
-      *(lptr<f32x4_t>)(smem + at32(r, cl)) = f32x4_t{x[0], x[1], x[2], x[3]};
-      *(lptr<f32x4_t>)(smem + at32(r, cl + 4)) = f32x4_t{x[4], x[5], x[6], x[7]};
     } else {
       const u32x4 v = *(gptr<const u32x4>)(a.codes + blk_index(row, c, a.ldc));
       const float m = c < a.v ? a.gm[(c >> a.group_shift) * a.gstep + row * a.rstep] : 0.0f;
@@ -1168,8 +1177,12 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
         const float p = q == 65535u ? 0.0f : __builtin_amdgcn_exp2f(base - float(q) * (kLossOctaves / 65535.0f));
         x[e] = rw.z != 0.0f && c + e < a.v ? p * f : 0.0f;
       }
-      *(lptr<u32x4>)(smem + at16(r, cl)) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                                                 pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+    }
+    if constexpr (WIDE) {
+      *(lptr<f32x4_t>)(smem + at32(r, cl)) = f32x4_t{x[0], x[1], x[2], x[3]};
+      *(lptr<f32x4_t>)(smem + at32(r, cl + 4)) = f32x4_t{x[4], x[5], x[6], x[7]};
+    } else {
+      *(lptr<u32x4>)(smem + at16(r, cl)) = pack8(x);
     }
   }
   __syncthreads();
@@ -1182,7 +1195,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
     if (rw.z == 0.0f) return;
     const float q = a.q[r0 * a.k + i], d = a.zt[r0 * a.k + i] - rw.x, e = expf(d);
     const float x = rw.z * (target_pq(q, d, e, rw.y) + rw.w * e) / (1.0f + rw.y);
-    if constexpr (F32) *(lptr<float>)(smem + at32(r, id)) = x;
+    if constexpr (WIDE) *(lptr<float>)(smem + at32(r, id)) = x;
     else *(lptr<uint16_t>)(smem + at16(r, id)) = uint16_t(pack_bf16x2(x, 0.0f));
   };
   for (int i = t; i < 32 * a.k; i += 8 * 256) {  // eight ids asked for at a time
@@ -1206,13 +1219,14 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   for (int it = 0; it < 4; ++it) {
     const int r = crow(it), cl = ccol(it);
     uint16_t* dst = a.dz + blk_index(r0 + r, c0 + cl, a.ldc);
-    if constexpr (F32) {
+    if constexpr (WIDE) {
       const f32x4_t v0 = *(lptr<f32x4_t>)(smem + at32(r, cl)), v1 = *(lptr<f32x4_t>)(smem + at32(r, cl + 4));
       float x[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= scales[it];
+      for (int e = 0; e < 8; ++e)
+        if constexpr (F32) x[e] *= scales[it];
 #pragma unroll
-      for (int part = 0; part < 2; ++part) *(gptr<u32x4>)(dst + part * a.dz_part) = split8(x);
+      for (int part = 0; part < 2; ++part) *(gptr<u32x4>)(dst + part * a.dz_part) = F32 ? split8(x) : split8_bf16(x);
     } else {
       *(gptr<u32x4>)dst = *(lptr<u32x4>)(smem + at16(r, cl));
     }
@@ -1262,20 +1276,21 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
 }
 
 // Products for at most 32 MI tokens (LossStream). Eight waves; K in steps through a ring of NST stages filled NST - 1 steps
-// ahead by direct loads. Bound by HBM: w is read once, 32 KiB per step, with up to (NST - 1) steps of it in flight per CU.
+// ahead by direct loads. Bound by HBM: w is read once, QB bytes per step, with up to (NST - 1) steps of it in flight per CU.
 // logits: a stage holds QR rows of w by KT of h; a wave takes all tokens by 32 rows of w, and half of the step's K where QR = 128
 //   (the halves are added in LDS at the tile's end). 128 rows of 256 bytes rather than 256 of 128: a head of 128256 x 4096 is read
 //   in 215 us (4.9 TB/s) instead of 227; more tokens leave no room for it.
-// dx: 64 rows of w by 256 of h, a wave 32 columns; chunk c of row r in slot c ^ 2 (r % 4); fragments read transposed.
+// dx: KT rows of w by 256 of h, a wave 32 columns; chunk c of row r in slot c ^ 2 (r % 4); fragments read transposed.
 // Past a row's end lie the next row's values, past w's end its last ones: they meet zeros of x or dz, or belong to columns
 // that are not stored.
 template <int MI, int KIND>
 __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a) {
-  constexpr int QR = stream_rows(MI), KT = KIND == kLossLogits ? 16384 / QR : 64;  // (dx: QR is not used)
-  constexpr int KB = KT / 32, PB = MI * 32 * KT * 2, QB = 32768, STAGE = PB + QB;
+  constexpr int QR = stream_rows(MI), KT = KIND == kLossLogits ? 16384 / QR : stream_step(MI);  // (dx: QR is not used)
+  constexpr int PP = KIND == kLossLogits ? 1 : 2;  // parts of P
+  constexpr int KB = KT / 32, PPB = MI * 32 * KT * 2, PB = PP * PPB, QB = KIND == kLossLogits ? 32768 : KT * 512, STAGE = PB + QB;
   constexpr int NST = 160 * 1024 / STAGE < 4 ? 160 * 1024 / STAGE : 4;
-  constexpr int PBLK = MI * 2 * KB;                            // 1 KiB blocks of P per step
-  constexpr int PL = PBLK < 8 ? 1 : PBLK / 8, LOADS = PL + 4;  // per wave and step (four blocks: two waves load the same)
+  constexpr int PBLK = PP * MI * 2 * KB;                            // 1 KiB blocks of P per step
+  constexpr int PL = PBLK < 8 ? 1 : PBLK / 8, QL = QB / 8192, LOADS = PL + QL;  // per wave and step (four blocks: two waves load the same)
   static_assert(NST >= 2 && NST * STAGE <= 160 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[NST * STAGE];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1300,13 +1315,14 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
     const __amdgpu_buffer_rsrc_t pr = __builtin_amdgcn_make_buffer_rsrc((void*)a.P, 0, 0xffffffffu, 0x00020000);
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      const int b = (i * 8 + w) % PBLK, kb = b / (MI * 2), panel = b % (MI * 2);  // K block of 32, 16-row panel
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, sb + kb * (MI * 2048) + panel * 1024, 16, ploff,
-                                               uint32_t(panel) * uint32_t(a.ldp * 32) + uint32_t(k * KB + kb) * 1024u, 0, 0);
+      const int b = (i * 8 + w) % PBLK, part = b / (MI * 2 * KB), kb = b / (MI * 2) % KB, panel = b % (MI * 2);  // kb: of 32; panel: 16 rows
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          pr, sb + b * 1024, 16, ploff,
+          uint32_t(part) * uint32_t(a.ppart * 2) + uint32_t(panel) * uint32_t(a.ldp * 32) + uint32_t(k * KB + kb) * 1024u, 0, 0);
     }
-    const __amdgpu_buffer_rsrc_t qr = rows_from(KIND == kLossLogits ? int64_t(tile) * QR : int64_t(k) * 64);
+    const __amdgpu_buffer_rsrc_t qr = rows_from(KIND == kLossLogits ? int64_t(tile) * QR : int64_t(k) * KT);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {  // logits: rows RPI (8 i + w) ..; dx: rows 2 (8 i + w), + 1
+    for (int i = 0; i < QL; ++i) {  // logits: rows RPI (8 i + w) ..; dx: rows 2 (8 i + w), + 1
       const uint32_t at = KIND == kLossLogits ? uint32_t(i * 8 * RPI * wrow) + uint32_t(k) * uint32_t(KT * 2)
                                               : uint32_t(i * 16 * wrow) + uint32_t(tile) * 512u;
       const uint32_t off = qloff + at;
@@ -1340,7 +1356,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
       issue(tile, k0 + min(kt + NST - 1, nk - 1), cs == 0 ? NST - 1 : cs - 1);
       const uint8_t* sb = smem + cs * STAGE;
 #pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) {  // 16 of K
+      for (int s4 = 0; s4 < (KIND == kLossLogits ? 4 : KT / 16); ++s4) {  // 16 of K
         const int sl = kh * 4 + s4;
         bf16x8_t qf;
         if constexpr (KIND == kLossLogits) {
@@ -1355,11 +1371,13 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
           qf = join_tr(lo, hi);
         }
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-          const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(sb + (sl >> 1) * (MI * 2048) + (i * 32 + fr) * kRowB +
-                                                                 ((((sl & 1) * 2 + fh) ^ swz(fr)) << 4));
-          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, pf, acc[i], 0, 0, 0);
-        }
+        for (int part = PP - 1; part >= 0; --part)
+#pragma unroll
+          for (int i = 0; i < MI; ++i) {
+            const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(sb + part * PPB + (sl >> 1) * (MI * 2048) + (i * 32 + fr) * kRowB +
+                                                                   ((((sl & 1) * 2 + fh) ^ swz(fr)) << 4));
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, pf, acc[i], 0, 0, 0);
+          }
       }
       cs = cs + 1 == NST ? 0 : cs + 1;
     }
@@ -1459,95 +1477,127 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
   LOSS_WAIT_VMCNT(0);
 }
 
-// dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). Many small workgroups instead of the
-// persistent kernel, whose tiles would each wait for one short load and one store after the other (48 tokens, 128256 x 4096: 247 us
-// for 1.05 GB, 295 there): four waves on 64 rows (ids) by 256 columns, all of K loaded at once, dz and x read transposed, the result through
-// LDS so that a wave stores whole rows of 512 bytes.
+// dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). A workgroup of four waves keeps CT columns
+// of x in registers and goes through blocks of 64 rows (ids), gridDim.y blocks apart: both parts of the next block of dz are on
+// their way while this one's product goes out, through LDS, so that a wave stores whole rows of CT columns. (48 tokens, 128256 x 4096,
+// 1.05 GB: DW48 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel more.)
 template <int KS>
 __global__ __launch_bounds__(256) void loss_dw_kernel(const LossGemm a) {
-  constexpr int NPAN = 2 * KS, PB = NPAN * 2048, QB = NPAN * 8192;  // panels of 16 tokens; dz and x in LDS
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[PB + QB > 32768 ? PB + QB : 32768];
+  constexpr int NPAN = 2 * KS, NJ = KS <= 2 ? 2 : 1, CT = 128 * NJ, CB = CT / 32;  // panels of 16 tokens; columns, in blocks of 32
+  constexpr int PPB = NPAN * 2048, PB = 2 * PPB, QB = NPAN * CB * 1024;            // dz's parts, x
+  constexpr int OUT = 2 * PB, XAT = PB;  // LDS: two blocks of dz, 32 rows of the result; x is first staged over the second and the third
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[OUT + 32 * CT * 2];
+  static_assert(XAT + QB <= OUT + 32 * CT * 2, "room for x");
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int bj = blockIdx.x % a.tn, bi = blockIdx.x / a.tn;
+  const int bj = blockIdx.x, blocks = (a.rows + 63) / 64;
   const uint32_t loff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
-  const __amdgpu_buffer_rsrc_t pr =
-      __builtin_amdgcn_make_buffer_rsrc((void*)(a.P + int64_t(bi) * 1024), 0, 0xffffffffu, 0x00020000);
+  auto issue = [&](int bi, int at) {
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const __amdgpu_buffer_rsrc_t pr =
+          __builtin_amdgcn_make_buffer_rsrc((void*)(a.P + part * a.ppart + int64_t(bi) * 1024), 0, 0xffffffffu, 0x00020000);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {  // panel b / 2, block b % 2
+        const int b = i * 4 + w;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, (lds_byte*)(smem + at + part * PPB + b * 1024), 16, loff,
+                                                 uint32_t(b >> 1) * uint32_t(a.ldp * 32) + (b & 1) * 1024, 0, 0);
+      }
+    }
+  };
+  int bi = blockIdx.y;  // (< blocks)
   const __amdgpu_buffer_rsrc_t qr =
-      __builtin_amdgcn_make_buffer_rsrc((void*)(a.Q + int64_t(bj) * 4096), 0, 0xffffffffu, 0x00020000);
+      __builtin_amdgcn_make_buffer_rsrc((void*)(a.Q + int64_t(bj) * (CT * 16)), 0, 0xffffffffu, 0x00020000);
 #pragma unroll
-  for (int i = 0; i < KS; ++i) {  // dz: panel b / 2, block b % 2
+  for (int i = 0; i < NPAN * CB / 4; ++i) {  // x: panel b / CB, block b % CB
     const int b = i * 4 + w;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(pr, (lds_byte*)(smem + b * 1024), 16, loff,
-                                             uint32_t(b >> 1) * uint32_t(a.ldp * 32) + (b & 1) * 1024, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_byte*)(smem + XAT + b * 1024), 16, loff,
+                                             uint32_t(b / CB) * uint32_t(a.ldq * 32) + (b % CB) * 1024, 0, 0);
   }
-#pragma unroll
-  for (int i = 0; i < NPAN * 2; ++i) {  // x: panel b / 8, block b % 8
-    const int b = i * 4 + w;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(qr, (lds_byte*)(smem + PB + b * 1024), 16, loff,
-                                             uint32_t(b >> 3) * uint32_t(a.ldq * 32) + (b & 7) * 1024, 0, 0);
-  }
+  issue(bi, 0);
   const float f = out_factor(a.alpha, a.denom);
-  f32x16_t acc[2][2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
   const int trow = (lane >> 5) * 8 + ((lane >> 2) & 3), tchunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1), tbyte = (lane & 1) * 8;
   const int tlo = trow * kRowB + ((tchunk ^ swz(trow)) << 4) + tbyte;
   const int thi = (trow + 4) * kRowB + ((tchunk ^ swz(trow + 4)) << 4) + tbyte;
   auto frag = [&](int at) {
-    lds_byte* q = (lds_byte*)(smem + at);
+    lds_byte* q = (lds_byte*)smem + at;
     return join_tr(read_tr((lptr<bf16x4_t>)(q + tlo)), read_tr((lptr<bf16x4_t>)(q + thi)));
   };
   LOSS_WAIT_VMCNT(0);
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
+  bf16x8_t qf[NPAN][NJ];
 #pragma unroll
-  for (int s = 0; s < NPAN; ++s) {
-    bf16x8_t pf[2], qf[2];
+  for (int s = 0; s < NPAN; ++s)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) pf[i] = frag((s * 2 + i) * 1024);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) qf[j] = frag(PB + (s * 8 + w * 2 + j) * 1024);
+    for (int j = 0; j < NJ; ++j) qf[s][j] = frag(XAT + (s * CB + w * NJ + j) * 1024);
+  LOSS_WAIT_LGKM0();
+  __builtin_amdgcn_sched_barrier(0);
+  constexpr int SL = CT / 8, RPI = 64 / SL, STORES = 16 / RPI;  // 16-byte slots of a row, XORed by the row; rows per store; a wave's stores per block
+  auto slot = [](int r, int sl) { return OUT + r * (CT * 2) + ((sl ^ r) & (SL - 1)) * 16; };
+  const int er = lane & 31, eh = lane >> 5;
+  for (int at = 0;; at ^= PB) {
+    __builtin_amdgcn_s_barrier();  // this block of dz is there for all waves, the other one's place is free
+    const int next = bi + gridDim.y;
+    if (next < blocks) issue(next, at ^ PB);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16_t acc[2][NJ];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], pf[i], acc[i][j], 0, 0, 0);
-  }
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_barrier();  // (the fragments are read: the products need them)
-  // 64 rows of 512 bytes, 16-byte slots XORed by the row
-  const int er = lane & 31, eh = lane >> 5;
-  auto at = [](int r, int sl) { return r * 512 + ((sl ^ r) & 31) * 16; };
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const f32x16_t& v = acc[i][p >> 2];
-      const int o = 4 * (p & 3);
-      *(lptr<u32x2>)((lds_byte*)smem + at(i * 32 + er, w * 8 + (p >> 2) * 4 + (p & 3)) + eh * 8) =
-          u32x2{pack_bf16x2(v[o] * f, v[o + 1] * f), pack_bf16x2(v[o + 2] * f, v[o + 3] * f)};
-    }
-  LOSS_WAIT_LGKM0();
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
+    for (int part = 1; part >= 0; --part)  // (the order of the tiles' kernel: dw is the same with dx and without)
 #pragma unroll
-  for (int it = 0; it < 8; ++it) {
-    const int r = w * 16 + it * 2 + eh;
-    const u32x4 val = *(lptr<u32x4>)((lds_byte*)smem + at(r, er));
-    const int row = bi * 64 + r, c = bj * 256 + er * 8;
-    if (row < a.rows) {
-      uint16_t* dst = (uint16_t*)a.out + int64_t(row) * a.ldo + c;
-      if (c + 8 <= a.cols) {
-        *(gptr<u32x4_a2>)dst = val;
-      } else {
+      for (int s = 0; s < NPAN; ++s) {
+        bf16x8_t pf[2];
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-          if (c + t < a.cols) *(gptr<uint16_t>)(dst + t) = uint16_t(val[t >> 1] >> (16 * (t & 1)));
+        for (int i = 0; i < 2; ++i) pf[i] = frag(at + part * PPB + (s * 2 + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[s][j], pf[i], acc[i][j], 0, 0, 0);
       }
-    }
+    static_for<2>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+#pragma unroll
+      for (int p = 0; p < 4 * NJ; ++p) {
+        const f32x16_t& v = acc[i][p >> 2];
+        const int o = 4 * (p & 3);
+        *(lptr<u32x2>)((lds_byte*)smem + slot(er, (w * NJ + (p >> 2)) * 4 + (p & 3)) + eh * 8) =
+            u32x2{pack_bf16x2(v[o] * f, v[o + 1] * f), pack_bf16x2(v[o + 2] * f, v[o + 3] * f)};
+      }
+      LOSS_WAIT_LGKM0();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int it = 0; it < STORES / 2; ++it) {
+        const int r = w * 8 + it * RPI + lane / SL, sl = lane % SL;
+        const u32x4 val = *(lptr<u32x4>)((lds_byte*)smem + slot(r, sl));
+        const int row = bi * 64 + i * 32 + r, c = bj * CT + sl * 8;
+        if (row < a.rows) {
+          uint16_t* dst = (uint16_t*)a.out + int64_t(row) * a.ldo + c;
+          if (c + 8 <= a.cols) {
+            *(gptr<u32x4_a2>)dst = val;
+          } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+              if (c + t < a.cols) *(gptr<uint16_t>)(dst + t) = uint16_t(val[t >> 1] >> (16 * (t & 1)));
+          }
+        }
+      }
+      LOSS_WAIT_LGKM0();
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (i == 0) __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (next >= blocks) break;
+    // the next block of dz: behind its loads come this block's stores, STORES of them where no row or column is cut off
+    if (bj * CT + CT <= a.cols) LOSS_WAIT_VMCNT(STORES);
+    else LOSS_WAIT_VMCNT(0);
+    bi = next;
   }
 }
 
@@ -1602,6 +1652,8 @@ void launch_gemm_seg(const LossGemm2& a, hipStream_t st) {
   const dim3 grid(kGemmXcds * Grid<NW, TB>::SLOTS), block(NW * 64);
   if (a.g[0].nseg == 1)
     hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, 1, KIND>), grid, block, 0, st, a);
+  else if (KIND == kLossOut && a.g[0].nseg == 2)
+    hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, 2, kLossOut>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((loss_gemm_kernel<NW, TB, kLossMaxSeg, KIND>), grid, block, 0, st, a);
 }
@@ -1647,9 +1699,11 @@ hipError_t launch_loss_grad(const LossGrad& b, hipStream_t st) {
   a.x.blocks_begin = (a.rows_pad / 32) * (a.v_pad / 256) + (a.total.loss ? 1 : 0);
   const dim3 grid(unsigned(a.x.blocks_begin) + (a.x.src ? unsigned(a.rows_pad / 32) * unsigned(a.x.cols / 256) : 0u));
   if (a.logits)
-    hipLaunchKernelGGL(loss_grad_kernel<true>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((loss_grad_kernel<true, 2>), grid, dim3(256), 0, st, a);
+  else if (a.parts == 2)
+    hipLaunchKernelGGL((loss_grad_kernel<false, 2>), grid, dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL(loss_grad_kernel<false>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((loss_grad_kernel<false, 1>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -1677,7 +1731,10 @@ void launch_stream(const LossStream& a, int mi, hipStream_t st) {
 }
 
 hipError_t launch_loss_dw(const LossGemm& a, int steps, hipStream_t st) {
-  const dim3 grid(unsigned((a.rows + 63) / 64) * unsigned(a.tn)), block(256);
+  const int columns = steps <= 2 ? 256 : 128, tn = (a.cols + columns - 1) / columns, blocks = (a.rows + 63) / 64;
+  // three workgroups per CU (two where LDS holds no more) in one round, of as many blocks each
+  const int slots = (steps <= 2 ? 3 : 2) * 256 / tn, each = slots > 0 ? (blocks + slots - 1) / slots : blocks;
+  const dim3 grid(unsigned(tn), unsigned((blocks + each - 1) / each)), block(256);
   if (steps == 1) hipLaunchKernelGGL(loss_dw_kernel<1>, grid, block, 0, st, a);
   else if (steps == 2) hipLaunchKernelGGL(loss_dw_kernel<2>, grid, block, 0, st, a);
   else hipLaunchKernelGGL(loss_dw_kernel<4>, grid, block, 0, st, a);

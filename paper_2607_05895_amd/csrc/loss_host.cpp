@@ -53,7 +53,8 @@ struct Plan {
   bool f32 = false, grads = false;
   bool copy = false;            // w is read from a bf16 copy
   int stream = 0;               // rows / 32 of the products for a few tokens, or 0
-  int parts = 1, nseg = 1;
+  int parts = 1, dz_parts = 1;  // of x and w, of dz
+  int nseg = 1, out_nseg = 1;   // pairs of parts: of the logits, of dx and dw
   int64_t n = 0, v = 0, h = 0, k = 1;
   int64_t chunk = 0, n_pad = 0, vp = 0, hk = 0, hp = 0, ldw = 0;
   int group = kLossGroup;       // columns of a softmax partial
@@ -156,7 +157,9 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.f32 = a->dtype == MFSDP_F32;
   p.grads = a->dx || a->dw;
   p.parts = p.f32 ? 2 : 1;
+  p.dz_parts = p.f32 || a->n <= kStreamTokens ? 2 : 1;
   p.nseg = p.f32 ? kLossMaxSeg : 1;
+  p.out_nseg = p.f32 ? kLossMaxSeg : p.dz_parts;
   p.n = a->n;
   p.v = a->v;
   p.h = a->h;
@@ -185,7 +188,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   if (p.stream) {
     if (a->dx) {
       // a workgroup per CU, in ranges of at least eight steps
-      const int64_t steps = up(p.v, 64) / 64, tiles = p.hp / 256;
+      const int64_t kt = stream_step(p.stream), steps = up(p.v, kt) / kt, tiles = p.hp / 256;
       const int64_t splits = std::max<int64_t>(1, std::min(steps / 8, (256 + tiles - 1) / tiles));
       p.dx.nk = int(steps);
       p.dx.tn = int(tiles);
@@ -197,13 +200,13 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
     p.logits = choose(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.nseg * p.hk / 32);
     p.logits.nk = int(p.hk / 32);
   }
-  const int64_t wsteps = p.nseg * up(std::min(p.chunk, std::max<int64_t>(p.n, 1)), 32) / 32;
+  const int64_t wsteps = p.out_nseg * up(std::min(p.chunk, std::max<int64_t>(p.n, 1)), 32) / 32;
   if (a->dx && !p.stream) {
-    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.nseg * vsteps, a->dw ? wsteps : 0, p.dx, p.dw);
+    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.out_nseg * vsteps, a->dw ? wsteps : 0, p.dx, p.dw);
     p.dx.nk = int(vsteps);
     // room for the ranges of dx alone too: a call with fewer outputs never needs more workspace
     Gemm alone, none;
-    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.nseg * vsteps, 0, alone, none);
+    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.out_nseg * vsteps, 0, alone, none);
     for (const Gemm& g : {p.dx, alone})
       if (g.splits > 1) part = std::max(part, size_t(g.items()) * size_t(g.tile) * g.tile * 4);
   } else if (a->dw) {
@@ -237,7 +240,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.xb = take(p.chunk * p.hp * es);
   if (p.copy) p.wb = take(p.v * p.ldw * es);
   if (p.grads) {
-    p.codes = take(p.chunk * p.vp * es);
+    p.codes = take(p.chunk * p.vp * 2 * p.dz_parts);
     if (p.f32) p.z32 = take(p.chunk * p.vp * 4);
   }
   p.part = take(int64_t(part));
@@ -288,7 +291,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
   const int64_t xpart = p.chunk * p.hp, wpart = p.v * p.ldw, dzpart = p.chunk * p.vp;
   const uint16_t* const w = p.copy ? u16p(p.wb) : static_cast<const uint16_t*>(a->w);
   // P Q^T with Q = w (row-major) or x (panel blocked)
-  auto product = [&](const Gemm& g, size_t P, int64_t ldp, int64_t ppart, bool of_w, int nk) {
+  auto product = [&](const Gemm& g, size_t P, int64_t ldp, int64_t ppart, int nseg, bool of_w, int nk) {
     LossGemm m{};
     m.P = u16p(P);
     m.ldp = ldp;
@@ -298,10 +301,10 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     m.qrows = p.v;
     m.qpart = of_w ? wpart : xpart;
     m.unscale = f32p(p.inv) + (of_w ? 1 : 0);
-    m.nseg = p.nseg;
+    m.nseg = nseg;
     m.nk = nk;
-    m.kper = g.splits > 1 ? g.kper : p.nseg * nk;
-    m.splits = (p.nseg * nk + m.kper - 1) / m.kper;
+    m.kper = g.splits > 1 ? g.kper : nseg * nk;
+    m.splits = (nseg * nk + m.kper - 1) / m.kper;
     m.tm = g.tm;
     m.tn = g.tn;
     return m;
@@ -377,7 +380,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     } else {
       LossGemm2 zz{};
       LossGemm& z = zz.g[0];
-      z = product(p.logits, p.xb, p.hp, xpart, true, p.logits.nk);
+      z = product(p.logits, p.xb, p.hp, xpart, p.nseg, true, p.logits.nk);
       zz.count = 1;
       zz.queue = prep.queues;
       z.tm = int(up(rows, p.logits.tile) / p.logits.tile);
@@ -440,6 +443,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
     gr.ldc = p.vp;
     gr.dz = u16p(p.codes);
     gr.dz_part = dzpart;
+    gr.parts = p.dz_parts;
     gr.gm = rw.gm;
     gr.gstep = p.gstep;
     gr.rstep = p.rstep;
@@ -467,7 +471,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
 
     LossGemm mx{}, mw{};
     if (a->dx && !p.stream) {
-      mx = product(p.dx, p.codes, p.vp, dzpart, true, p.dx.nk);
+      mx = product(p.dx, p.codes, p.vp, dzpart, p.out_nseg, true, p.dx.nk);
       mx.op = kLossDx;
       mx.row_most = rw.row_most;
       mx.tm = int(up(rows, p.dx.tile) / p.dx.tile);
@@ -481,7 +485,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (mx.splits > 1) mx.part = f32p(p.part);
     }
     if (a->dw) {
-      mw = product(p.dw, p.codes, p.vp, dzpart, false, int(up(rows, 32) / 32));
+      mw = product(p.dw, p.codes, p.vp, dzpart, p.out_nseg, false, int(up(rows, 32) / 32));
       mw.op = kLossDw;
       mw.rows = int(p.v);
       mw.cols = int(p.h);
@@ -505,6 +509,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       s.P = u16p(p.codes);
       s.w = w;
       s.ldp = p.vp;
+      s.ppart = dzpart;
       s.v = p.v;
       s.h = p.h;
       s.nk = p.dx.nk;
@@ -522,7 +527,6 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       LOSS_TRY(launch_loss_gemm(both, kLossOut, p.dx.tile, st), "dx launch");
     }
     if (a->dw && short_dw) {
-      mw.tn = int(p.hp / 256);
       LOSS_TRY(launch_loss_dw(mw, rows <= 32 ? 1 : rows <= 64 ? 2 : 4, st), "dw launch");
     } else if (a->dw && !together) {
       both.g[0] = mw;

@@ -12,6 +12,10 @@
 // w, and one per row of x and of dz, so that no token's digits depend on another token. For dw, which sums over the tokens, x is
 // split a second time, its rows divided by dz's scales. Values that are not finite are left out of the scales.
 //
+// dz of bf16 inputs is rounded to bf16. Up to 128 tokens it is held in two bf16 parts instead (its products run over both, one K
+// segment each): there one rounding of a target's dz is a share of a whole row of dx and dw that no other token evens out (up to 2^-8,
+// beside the results' own rounding), and the second part costs next to nothing where reading w and writing dw take the time.
+//
 // Between the logits and their gradient a chunk of bf16 inputs holds each logit in 16 bits: the distance
 // from the largest of its row in its 64 columns, in steps of 64 / 65535 of a factor of two. That is a relative error of p of
 // at most half a step times ln 2 = 3.4e-4, a sixth of the rounding of dz to bf16 that follows, at half the bytes of fp32, and
@@ -43,7 +47,7 @@ struct LossGemm {
   int64_t ldp, ldq, qrows;
   int64_t ppart, qpart;                            // elements between the parts
   const float *row_most, *unscale;                 // fp32: what the scales of P's rows come from (null: no scale), 1 / the scale of Q
-  int32_t nseg, nk, splits, kper;
+  int32_t nseg, nk, splits, kper;                  // nseg: 1; 2: P in two bf16 parts; 3: both in two fp16 parts
   int32_t tm, tn;                                  // tiles
   int32_t rows, cols;                              // real rows and columns of the result
   int32_t op;                                      // kLossDx, kLossDw (gradients)
@@ -76,10 +80,12 @@ struct LossGemm2 {
 
 // Products for a few tokens (at most 32 MI), where reading w counts: w is read as it lies, once, with no packed copy.
 //   logits: tiles of stream_rows(MI) ids, K = h in steps of 16384 / stream_rows;  dx: tiles of 256 columns of h, K = v in steps of
-//   64, cut into `splits` ranges of kper steps, whose fp32 results lie row-major (32 MI x ldo) one after another in part.
+//   stream_step(MI), cut into `splits` ranges of kper steps, whose fp32 results lie row-major (32 MI x ldo) one after another in part.
 __host__ __device__ constexpr int stream_rows(int mi) { return mi <= 2 ? 128 : 256; }
+__host__ __device__ constexpr int stream_step(int mi) { return mi <= 2 ? 64 : 32; }
 struct LossStream {
-  const uint16_t *P, *w;     // P: x, or dz; panel blocked with ldp columns
+  const uint16_t *P, *w;     // P: x, or dz (two parts, ppart elements apart); panel blocked with ldp columns
+  int64_t ppart;
   int64_t ldp, v, h;
   int32_t nk, tiles, splits, kper;
   float inv_t;
@@ -173,14 +179,15 @@ struct LossRows {
 };
 
 // dz of a chunk, without the factor scale / (T D) common to all tokens (which the products apply: rounded with it, the
-// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place, or fp32
-// logits -> two fp16 parts, each row scaled.
+// -1 of every label would be off by the same share of a bf16 step): codes -> bf16 in place (and a second part elsewhere), or
+// fp32 logits -> two fp16 parts, each row scaled.
 struct LossGrad {
   uint16_t* codes;
   const float* logits;
   int64_t ldc;
   uint16_t* dz;                // (codes: dz = codes)
   int64_t dz_part;
+  int32_t parts;               // of dz
   const float* gm;
   int64_t gstep, rstep;
   const float4* row;
