@@ -541,23 +541,29 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           a.gm[at] = m * inv_t;
           a.gs[at] = s + (ones - 1.0f);
         }
-        auto target = [&](int id, int j) {
-          const int x = (id - c0) ^ (eh << 2);  // in this lane's columns: bits 0, 1, 3, 4, 5
-          if ((x & ~0x3b) == 0) {
+        // The row's targets in this lane's columns (bits 0, 1, 3, 4, 5 of the distance from the first): found 16 at a time, then
+        // taken one by one, with their ids read again (one place in the code: a small call spends its time on fetching instructions).
+        const auto place = [&](int id) { return (id - c0) ^ (eh << 2); };
+        for (int j0 = 0; j0 < a.k; j0 += 16) {
+          uint32_t hits = 0;
+          if (j0 == 0) hits = (place(id0[mi]) & ~0x3b) == 0;
+          if (a.k > 1) {
+            int id[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) id[i] = j0 + i < a.k ? *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j0 + i) : -1;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) hits |= (place(id[i]) & ~0x3b) == 0 ? 1u << i : 0u;
+          }
+          while (hits) {
+            const int j = j0 + __builtin_ctz(hits);
+            hits &= hits - 1;
+            const int x = place(j == 0 ? id0[mi] : *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j));
             const int e = (x >> 5) * 16 + ((x >> 3) & 3) * 4 + (x & 3);
             float z = 0.0f;
 #pragma unroll
             for (int f = 0; f < 32; ++f) z = e == f ? u[f] : z;
             a.zt[int64_t(row) * a.k + j] = z * inv_t;
           }
-        };
-        target(id0[mi], 0);
-        for (int j = 1; j < a.k; j += 16) {
-          int id[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) id[i] = j + i < a.k ? *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j + i) : -1;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) target(id[i], j + i);
         }
         if (F16 && a.logits) {
           float* dst = a.logits + int64_t(row) * a.ldc + c0;
@@ -878,18 +884,6 @@ __device__ __forceinline__ void pack_tile(const LossLabels& l, const LossPack& d
   const int64_t i = int(blockIdx.x) - d.blocks_begin;
   const int64_t tc = d.cols / 256, r0 = i / tc * 32, c0 = i % tc * 256;
   const int t = threadIdx.x, ch = t & 31;
-  uint32_t skip = 0;  // rows of the tile whose token does not count
-  if (d.label_row >= 0) {
-    if (t < 32) counts[t] = 0;
-    __syncthreads();
-    for (int e = t; e < 32 * l.k; e += 256) {
-      const int r = e / l.k;
-      if (r0 + r < d.R && slot_counts(l, (d.label_row + r0 + r) * l.k + (e - r * l.k))) counts[r] = 1;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int it = 0; it < 4; ++it) skip |= counts[it * 8 + (t >> 5)] ? 0u : 1u << it;
-  }
   const int64_t c = c0 + ch * 8;
   float x[4][8];
 #pragma unroll
@@ -897,7 +891,7 @@ __device__ __forceinline__ void pack_tile(const LossLabels& l, const LossPack& d
     const int64_t r = r0 + it * 8 + (t >> 5);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[it][e] = 0.0f;
-    if (r < d.R && c < d.C && !(skip >> it & 1)) {
+    if (r < d.R && c < d.C) {
       const int64_t at = r * d.C + c;
       if (d.bf16) {
         const uint16_t* p = (const uint16_t*)d.src + at;
@@ -930,6 +924,22 @@ __device__ __forceinline__ void pack_tile(const LossLabels& l, const LossPack& d
       }
     }
   }
+  uint32_t skip = 0;  // rows of the tile whose token does not count
+  if (d.label_row >= 0) {
+    if (t < 32) counts[t] = 0;
+    __syncthreads();
+    for (int e = t; e < 32 * l.k; e += 256) {
+      const int r = e / l.k;
+      if (r0 + r < d.R && slot_counts(l, (d.label_row + r0 + r) * l.k + (e - r * l.k))) counts[r] = 1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int it = 0; it < 4; ++it) skip |= counts[it * 8 + (t >> 5)] ? 0u : 1u << it;
+  }
+#pragma unroll
+  for (int it = 0; it < 4; ++it)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[it][e] = skip >> it & 1 ? 0.0f : x[it][e];
   if (!d.bf16) {
     float all = 1.0f, inv;
     if (d.most) {
@@ -1021,6 +1031,10 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
     // (asked for here, needed at the end)
     const bool mine = gl == 0 && r < a.rows;
     const float on = mine ? a.on[r] : 0.0f, ent = mine ? a.ent[r] : 0.0f, wt = mine && a.weight ? a.weight[r] : 1.0f;
+    // this thread's first target
+    const bool aims = r < a.rows && gl < a.k;
+    const float q0 = aims ? a.q[r * a.k + gl] : 0.0f, z0 = aims ? a.zt[r * a.k + gl] : 0.0f;
+    const int id0 = aims ? a.id[r * a.k + gl] : -1;
     for (int g = gl; g < (r < a.rows ? a.groups : 0); g += BATCH * GS) {
       float gm[BATCH], gs[BATCH];
 #pragma unroll
@@ -1042,20 +1056,30 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
       ss[w][rl] = s;
     }
     __syncthreads();
-    if (gl == 0) {
-      for (int i = 1; i < 16; ++i) join_softmax(m, s, sm[i][rl], ss[i][rl]);
-      sm[0][rl] = m;
-      ss[0][rl] = s;
+    if constexpr (RPB == 1) {  // every wave joins the waves' results by itself
+      m = sm[threadIdx.x & 15][0];
+      s = ss[threadIdx.x & 15][0];
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) join_softmax(m, s, __shfl_xor(m, o), __shfl_xor(s, o));
+    } else {
+      if (gl == 0) {
+        for (int i = 1; i < 16; ++i) join_softmax(m, s, sm[i][rl], ss[i][rl]);
+        sm[0][rl] = m;
+        ss[0][rl] = s;
+      }
+      __syncthreads();
+      m = sm[0][rl];
+      s = ss[0][rl];
     }
-    __syncthreads();
     // sum of q (m - z) over the row's targets; a bound on |dz| at them, in units of 1 / (1 + s); whether one of them is the largest
-    const float top = sm[0][rl], others = ss[0][rl];
+    const float top = m, others = s;
     const float lz = 2.0f * a.z_loss * (top + log1pf(others));
     float d = 0.0f, bound = 0.0f;
     bool of_top = false;
     for (int j = gl; j < (r < a.rows ? a.k : 0); j += GS) {
-      const float q = a.q[r * a.k + j], z = a.zt[r * a.k + j];
-      if (q > 0.0f && a.id[r * a.k + j] >= 0) {
+      const bool f = j == gl;
+      const float q = f ? q0 : a.q[r * a.k + j], z = f ? z0 : a.zt[r * a.k + j];
+      if (q > 0.0f && (f ? id0 : a.id[r * a.k + j]) >= 0) {
         d += q * (top - z);
         if (a.most) {
           const float e = expf(z - top);
@@ -1149,6 +1173,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   }
   const int64_t r0 = int64_t(blockIdx.x / tc) * 32, c0 = int64_t(blockIdx.x % tc) * 256;
   const int t = threadIdx.x, ln = t & 63, w = t >> 6;
+  const int first_id = t < 32 * a.k ? a.id[r0 * a.k + t] : -1;
   // chunk (row, 8 columns) it of a thread, as its 1 KiB block lies: lane: row lane / 4, chunk lane % 4
   auto crow = [&](int it) { return (it >> 1) * 16 + (ln >> 2); };
   auto ccol = [&](int it) { return (w * 2 + (it & 1)) * 32 + (ln & 3) * 8; };
@@ -1201,7 +1226,8 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const LossGrad a) {
   for (int i = t; i < 32 * a.k; i += 8 * 256) {  // eight ids asked for at a time
     int id[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) id[e] = i + e * 256 < 32 * a.k ? a.id[r0 * a.k + i + e * 256] : -1;
+    for (int e = 0; e < 8; ++e)
+      id[e] = i == t && e == 0 ? first_id : i + e * 256 < 32 * a.k ? a.id[r0 * a.k + i + e * 256] : -1;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (id[e] >= 0) target(i + e * 256, id[e]);

@@ -408,6 +408,14 @@ def _stream() -> int:
 
 
 _FLOAT = ("bfloat16", "float32")
+_DTYPE_NAMES: dict = {}  # of torch dtypes
+
+
+def _dtype_name(dtype) -> str:
+    name = _DTYPE_NAMES.get(dtype)
+    if name is None:
+        name = _DTYPE_NAMES[dtype] = str(dtype).replace("torch.", "")
+    return name
 
 
 def _ptr(t, what: str, shape=None, dtypes=_FLOAT) -> int:
@@ -420,13 +428,13 @@ def _ptr(t, what: str, shape=None, dtypes=_FLOAT) -> int:
         raise TypeError(f"{what}: expected a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda or t.layout != torch.strided:
         raise ValueError(f"{what}: must be a dense CUDA tensor, got {t.layout} on {t.device}")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{what}: is on {t.device} but the current device is cuda:{torch.cuda.current_device()}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
-    if str(t.dtype).replace("torch.", "") not in dtypes:
+    if _dtype_name(t.dtype) not in dtypes:
         raise TypeError(f"{what}: dtype must be one of {dtypes}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != tuple(shape):
         raise ValueError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is required")
     return t.data_ptr()
 
@@ -607,7 +615,7 @@ def head_loss_args_t(x, w, loss=None, token_loss=None, lse=None, dx=None, dw=Non
         raise ValueError(f"x and w: (n, h) and (v, h) are required, got {tuple(x.shape)} and {tuple(w.shape)}")
     n, h = x.shape
     v = w.shape[0]
-    f, same = ("float32",), (str(x.dtype).replace("torch.", ""),)
+    f, same = ("float32",), (_dtype_name(x.dtype),)
     opt = lambda t, what, shape, dts: _ptr(t, what, shape, dts) if t is not None else None  # noqa: E731
     xp = _ptr(x, "x")
     if loss is not None and loss.numel() != 1:
