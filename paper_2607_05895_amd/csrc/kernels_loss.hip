@@ -147,8 +147,10 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     return (ng - 1) * per - ((groups - 1) % kGemmXcds == x ? groups * per - total : 0) - taken;
   };
   bool home_out = false;
-  auto take = [&]() -> int {
-    gptr<int> q = (gptr<int>)b.queue;
+  gptr<int> q = (gptr<int>)b.queue;
+  auto ask = [&](int x) { return __hip_atomic_fetch_add(q + x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  auto item_of = [&](int x, int i) { return ((i / per + 1) * kGemmXcds + x) * per + i % per; };
+  auto take = [&](int i) -> int {  // i: what home's counter gave, if it was asked
     for (int x = home;;) {
       if (home_out) {
         int most = 0;
@@ -161,9 +163,9 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           }
         }
         if (most == 0) return -1;
+        i = ask(x);
       }
-      const int i = __hip_atomic_fetch_add(q + x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (left_in(x, i) > 0) return ((i / per + 1) * kGemmXcds + x) * per + i % per;
+      if (left_in(x, i) > 0) return item_of(x, i);
       home_out = true;
     }
   };
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   const bool asks = threadIdx.x == (NW - 1) * 64, queued = groups > kGemmXcds;
   bool has_next = false;
   if (queued) {
-    if (asks) mail[0] = take();
+    if (asks) mail[0] = take(ask(home));
     LOSS_WAIT_LGKM0();
     __builtin_amdgcn_s_barrier();
     has_next = item_at(__builtin_amdgcn_readfirstlane(mail[0]), nxt);
@@ -471,8 +473,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     LOSS_WAIT_VMCNT(0);
     __builtin_amdgcn_s_barrier();
     if (has_next && issuer) prologue(nxt);  // (leaves the last part of LDS to the epilogue)
-    int after = -1;  // the item after that: asked for here, needed at the epilogue's end
-    if (has_next && asks) after = take();
+    int after = 0;  // the item after that: home's counter is asked here and looked at behind the epilogue
+    if (has_next && asks && !home_out) after = ask(home);
 
     // acc[mi][ni][4 gg + t] of a lane is element (row, column) of the wave's part with row = 32 mi + lane % 32,
     // column = 32 ni + 8 gg + 4 (lane / 32) + t.
@@ -585,17 +587,15 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
             *(lptr<u32x2>)(slab + wr_base + (p >> 2) * 1024 + ((((p & 3) ^ wsw) - wsw) << 4)) =
                 u32x2{code2((u[o] - m) * C, (u[o + 1] - m) * C), code2((u[o + 2] - m) * C, (u[o + 3] - m) * C)};
           }
-          LOSS_WAIT_LGKM0();
-          __builtin_amdgcn_s_barrier();
+          // (the wave's own four blocks: its LDS writes and reads are in order, and no wave waits for another)
           const int rin = ln >> 2, ch = ln & 3;
 #pragma unroll
-          for (int b = 0; b < 4 * (TB / 32) / NW; ++b) {
-            const int blk = w * (4 * (TB / 32) / NW) + b, sp = blk / (TB / 32), cb = blk % (TB / 32);
+          for (int b = 0; b < 4; ++b) {
+            const int sp = wm * 2 + (b >> 1), cb = wn * 2 + (b & 1), blk = sp * (TB / 32) + cb;
             const u32x4 val = *(lptr<u32x4>)(slab + (blk << 10) + (rin << 6) + ((ch ^ swz(rin)) << 4));
             const int dr = (sp >> 1) * (MI * 32) + mi * 32 + (sp & 1) * 16 + rin;
             *(gptr<u32x4>)(a.codes + blk_index(int64_t(cur.bi) * TB + dr, int64_t(cur.bj) * TB + cb * 32 + ch * 8, a.ldc)) = val;
           }
-          __builtin_amdgcn_s_barrier();
         });
       }
     } else {
@@ -657,28 +657,23 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           }
         });
       } else {
-        // bf16, row-major, through the free stage: rounds of 32 rows of each wave row, whole row segments per store; 16-byte
-        // slots XORed by the row
-        constexpr int SL = TB / 8, ROWS = 64;
-        auto at = [](int r, int s) { return r * (TB * 2) + ((s ^ r) & (SL - 1)) * 16; };
+        // bf16, row-major, through the free stage: each wave its own 32 rows of 128 bytes at a time, whole lines per store, and
+        // no wave waits for another; 16-byte slots XORed by the row
+        const int slab_w = w * 4096;
+        auto at = [](int r, int s) { return r * 128 + ((s ^ r) & 7) * 16; };
         static_for<MI>([&](auto mi_c) {
           constexpr int mi = decltype(mi_c)::value;
-          const int sr = wm * 32 + er;
 #pragma unroll
           for (int p = 0; p < 8; ++p) {
             const f32x16_t& v = acc[mi][p >> 2];
             const int o = 4 * (p & 3);
-            *(lptr<u32x2>)(slab + at(sr, wn * 8 + (p >> 2) * 4 + (p & 3)) + eh * 8) =
-                u32x2{pack_bf16x2(v[o], v[o + 1]), pack_bf16x2(v[o + 2], v[o + 3])};
+            *(lptr<u32x2>)(slab + slab_w + at(er, p) + eh * 8) = u32x2{pack_bf16x2(v[o], v[o + 1]), pack_bf16x2(v[o + 2], v[o + 3])};
           }
-          LOSS_WAIT_LGKM0();
-          __builtin_amdgcn_s_barrier();
-          constexpr int RPI = 64 / SL, IT = ROWS / NW / RPI;  // rows per wave instruction, instructions
 #pragma unroll
-          for (int it = 0; it < IT; ++it) {
-            const int r = w * (ROWS / NW) + it * RPI + ln / SL, s = ln % SL;
-            const u32x4 val = *(lptr<u32x4>)(slab + at(r, s));
-            const int row = cur.bi * TB + (r >> 5) * (MI * 32) + mi * 32 + (r & 31), c = cur.bj * TB + s * 8;
+          for (int it = 0; it < 4; ++it) {
+            const int r = it * 8 + (ln >> 3), s = ln & 7;
+            const u32x4 val = *(lptr<u32x4>)(slab + slab_w + at(r, s));
+            const int row = cur.bi * TB + wm * (MI * 32) + mi * 32 + r, c = cur.bj * TB + wn * 64 + s * 8;
             if (row < a.rows) {
               uint16_t* dst = (uint16_t*)a.out + int64_t(row) * a.ldo + c;
               if (c + 8 <= a.cols) {
@@ -690,13 +685,15 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
               }
             }
           }
-          __builtin_amdgcn_s_barrier();
         });
       }
     }
+    // (every wave has left the last part of LDS)
+    LOSS_WAIT_LGKM0();
+    __builtin_amdgcn_s_barrier();
     if (!has_next) break;
     cur = nxt;
-    if (asks) mail[0] = after;
+    if (asks) mail[0] = take(after);
     LOSS_WAIT_LGKM0();
     __builtin_amdgcn_s_barrier();
     has_next = item_at(__builtin_amdgcn_readfirstlane(mail[0]), nxt);
@@ -1283,6 +1280,16 @@ __device__ __forceinline__ void store4(void* out, int bf16, int64_t at, f32x4_t 
   }
 }
 
+// s + ranges i .. i + 7 (as far as there are any), in order, all asked for before the first is added.
+__device__ __forceinline__ void add_ranges(f32x4_t& s, const float* p, int64_t stride, int i, int splits) {
+  f32x4_t v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = *(gptr<const f32x4_t>)(p + min(i + e, splits - 1) * stride);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (i + e < splits) s += v[e];
+}
+
 // The K ranges' partial tiles added in order; four elements per thread.
 template <int NW, int TB>
 __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
@@ -1291,7 +1298,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
   const int tile = blockIdx.x / (Q / 256), q = (blockIdx.x % (Q / 256)) * 256 + threadIdx.x;
   const float* p = a.part + int64_t(tile) * a.splits * (TB * TB) + q * 4;
   f32x4_t s = *(gptr<const f32x4_t>)p;
-  for (int i = 1; i < a.splits; ++i) s += *(gptr<const f32x4_t>)(p + int64_t(i) * (TB * TB));
+  for (int i = 1; i < a.splits; i += 8) add_ranges(s, p, TB * TB, i, a.splits);
   const int ln = q & 63, blk = (q >> 6) & (G::MI * G::NI * 4 - 1), w = (q >> 6) / (G::MI * G::NI * 4);
   const int bj = tile / a.tm, bi = tile - bj * a.tm;
   const int row = bi * TB + (w / G::WN) * (G::MI * 32) + (blk >> 3) * 32 + (ln & 31);
@@ -1636,7 +1643,7 @@ __global__ __launch_bounds__(256) void loss_join_rows_kernel(const LossJoin a) {
   if (row >= a.rows) return;
   const float* p = a.part + row * a.ldp + c;
   f32x4_t s = *(gptr<const f32x4_t>)p;
-  for (int i = 1; i < a.splits; ++i) s += *(gptr<const f32x4_t>)(p + i * a.stride);
+  for (int i = 1; i < a.splits; i += 8) add_ranges(s, p, a.stride, i, a.splits);
   s *= out_factor(a.alpha, a.denom);
   store4(a.out, a.out_bf16, row * a.ldo + c, s, a.cols - c);
 }
