@@ -418,18 +418,21 @@ def _dtype_name(dtype) -> str:
     return name
 
 
-def _ptr(t, what: str, shape=None, dtypes=_FLOAT) -> int:
+def _ptr(t, what: str, shape=None, dtypes=_FLOAT, device=None) -> int:
     """Data pointer of a tensor handed to the library, after checking what the C ABI cannot: that it
     is a dense, contiguous tensor on the current GPU (the calls run on that GPU's current stream)
     with the shape and dtype the call reads and writes. The library trusts pointers and sizes, so a
-    tensor that is smaller than the call assumes would be written past its end."""
+    tensor that is smaller than the call assumes would be written past its end. device: the current GPU, where
+    the caller has asked for it already."""
     import torch
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{what}: expected a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda or t.layout != torch.strided:
         raise ValueError(f"{what}: must be a dense CUDA tensor, got {t.layout} on {t.device}")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{what}: is on {t.device} but the current device is cuda:{torch.cuda.current_device()}")
+    if device is None:
+        device = torch.cuda.current_device()
+    if t.get_device() != device:
+        raise ValueError(f"{what}: is on {t.device} but the current device is cuda:{device}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
     if _dtype_name(t.dtype) not in dtypes:
@@ -439,8 +442,8 @@ def _ptr(t, what: str, shape=None, dtypes=_FLOAT) -> int:
     return t.data_ptr()
 
 
-def _ws(workspace) -> Tuple[int, int]:
-    return _ptr(workspace, "workspace", dtypes=("uint8",)), workspace.numel()
+def _ws(workspace, device=None) -> Tuple[int, int]:
+    return _ptr(workspace, "workspace", dtypes=("uint8",), device=device), workspace.numel()
 
 
 def muon_hparams(lr=0.02, weight_decay=0.0, momentum=0.95, nesterov=True, a=3.4445, b=-4.7750,
@@ -616,11 +619,12 @@ def head_loss_args_t(x, w, loss=None, token_loss=None, lse=None, dx=None, dw=Non
     n, h = x.shape
     v = w.shape[0]
     f, same = ("float32",), (_dtype_name(x.dtype),)
-    opt = lambda t, what, shape, dts: _ptr(t, what, shape, dts) if t is not None else None  # noqa: E731
     xp = _ptr(x, "x")
+    device = x.get_device()  # (the current one)
+    opt = lambda t, what, shape, dts: _ptr(t, what, shape, dts, device) if t is not None else None  # noqa: E731
     if loss is not None and loss.numel() != 1:
         raise ValueError(f"loss: one element is required, got shape {tuple(loss.shape)}")
-    return HeadLoss(xp, _ptr(w, "w", (v, h), same), n, v, h, _dt(x),
+    return HeadLoss(xp, _ptr(w, "w", (v, h), same, device), n, v, h, _dt(x),
                     _REDUCTIONS[reduction] if isinstance(reduction, str) else int(reduction), float(scale),
                     opt(token_weight, "token_weight", (n,), f), opt(loss, "loss", None, f),
                     opt(token_loss, "token_loss", (n,), f), opt(lse, "lse", (n,), f), opt(dx, "dx", (n, h), same),
@@ -637,10 +641,12 @@ def linear_xent_t(x, w, targets, loss=None, token_loss=None, lse=None, dx=None, 
     """Softmax cross entropy of x w^T with the labels `targets` (n, int64 or int32) into the outputs that are given, on
     torch's current stream. workspace: head_loss_workspace_t's tensor (None: allocated for this call)."""
     args = head_loss_args_t(x, w, loss, token_loss, lse, dx, dw, reduction, scale, token_weight, chunk_rows)
-    tp = _ptr(targets, "targets", (args.n,), _INT)
+    device = x.get_device()
+    tp = _ptr(targets, "targets", (args.n,), _INT, device)
     if workspace is None:
         workspace = head_loss_workspace_t(args, 1, x.device)
-    mfsdp_linear_xent(args, tp, targets.element_size(), int(ignore_index), float(z_loss), *_ws(workspace), _stream())
+    mfsdp_linear_xent(args, tp, targets.element_size(), int(ignore_index), float(z_loss), *_ws(workspace, device),
+                      _stream())
 
 
 def linear_distill_t(x, w, ids, logits, loss=None, token_loss=None, lse=None, dx=None, dw=None, temperature=1.0,
@@ -651,10 +657,12 @@ def linear_distill_t(x, w, ids, logits, loss=None, token_loss=None, lse=None, dx
     if ids.dim() != 2:
         raise ValueError(f"ids: (n, k) is required, got shape {tuple(ids.shape)}")
     k = ids.shape[1]
-    ip, lp = _ptr(ids, "ids", (args.n, k), _INT), _ptr(logits, "logits", (args.n, k))
+    device = x.get_device()
+    ip, lp = _ptr(ids, "ids", (args.n, k), _INT, device), _ptr(logits, "logits", (args.n, k), device=device)
     if workspace is None:
         workspace = head_loss_workspace_t(args, k, x.device)
-    mfsdp_linear_distill(args, ip, ids.element_size(), lp, _dt(logits), k, float(temperature), *_ws(workspace), _stream())
+    mfsdp_linear_distill(args, ip, ids.element_size(), lp, _dt(logits), k, float(temperature),
+                         *_ws(workspace, device), _stream())
 
 
 def scale_grad_t(grad, factor) -> None:
