@@ -132,7 +132,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / G::WN, wn = w % G::WN;
-  const int first = b.g[0].tm * b.g[0].tn * b.g[0].splits;
+  // (a launch that goes on from the sum over K ranges has one item per tile)
+  const int first = b.g[0].tm * b.g[0].tn * (KIND == kLossLogits && b.g[0].prev ? 1 : b.g[0].splits);
   const int total = first + (KIND == kLossOut && b.count > 1 ? b.g[1].tm * b.g[1].tn * b.g[1].splits : 0);
   const int per = min(G::SLOTS, (total + kGemmXcds - 1) / kGemmXcds);  // items of one group
   const int groups = (total + per - 1) / per;
@@ -279,17 +280,17 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   auto prologue = [&](const Item& it) {
     aim(it);
     if constexpr (KIND == kLossLogits) {
-      const int units = it.nk / 2;
+      const int units = it.nk / 2, u0 = it.k0 / 2;
 #pragma unroll
-      for (int i = 0; i < 2 * PL; ++i) issue_w(i, 0, kQAt);
+      for (int i = 0; i < 2 * PL; ++i) issue_w(i, u0, kQAt);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < PL; ++i) issue_p(i, s, s * HALF, std::false_type{});
+        for (int i = 0; i < PL; ++i) issue_p(i, it.k0 + s, s * HALF, std::false_type{});
 #pragma unroll
-      for (int i = 0; i < 2 * PL; ++i) issue_w(i, min(1, units - 1), kQAt + 2 * HALF);
+      for (int i = 0; i < 2 * PL; ++i) issue_w(i, u0 + min(1, units - 1), kQAt + 2 * HALF);
 #pragma unroll
-      for (int i = 0; i < PL; ++i) issue_p(i, min(2, it.nk - 1), 2 * HALF, std::false_type{});
+      for (int i = 0; i < PL; ++i) issue_p(i, it.k0 + min(2, it.nk - 1), 2 * HALF, std::false_type{});
     } else {
       auto steps = [&](auto trans_c) {
 #pragma unroll
@@ -337,9 +338,13 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   constexpr int NMF = MI * NI, NRD = MI + NI;  // MFMAs and fragments per 16-wide slice
   static_assert(DLOADS == NMF && PL == NMF / 2, "half of the loads in each half");
 
+  // logits in K ranges (small tiles only): the launch that goes on from their sum
+  constexpr bool RANGES = KIND == kLossLogits && TB == kLossTileSmall;
+  const bool summed = RANGES && b.g[0].prev;
+
   Item cur, nxt;
   if (!item_at(home * per + place, cur)) return;
-  if (issuer) prologue(cur);
+  if (issuer && !summed) prologue(cur);
   // (the last part of LDS is free whenever items are taken; the last wave asks: of eight waves it issues no loads to wait behind)
   int* mail = reinterpret_cast<int*>(smem + kSlabAt);
   const bool asks = threadIdx.x == (NW - 1) * 64, queued = groups > kGemmXcds;
@@ -397,10 +402,29 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         __builtin_amdgcn_sched_barrier(0);
       });
     };
+    // where this wave's part of a tile of sums lies: range 0 of the item's tile, in accumulator order
+    auto part_at = [&](int splits) {
+      return int64_t((cur.bj * b.g[cur.p].tm + cur.bi) * splits) * (TB * TB) + (w * MI * NI * 4 * 64 + lane) * 4;
+    };
+    auto load_sum = [&](const float* sum) {
+#pragma unroll
+      for (int q = 0; q < MI * NI * 4; ++q) {
+        const f32x4_t v = *(gptr<const f32x4_t>)(sum + q * 256);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[q / (NI * 4)][(q >> 2) & 1][4 * (q & 3) + t] = v[t];
+      }
+    };
+    auto store_part = [&](float* part) {
+#pragma unroll
+      for (int q = 0; q < MI * NI * 4; ++q) {
+        const f32x16_t& c = acc[q / (NI * 4)][(q >> 2) & 1];
+        *(gptr<f32x4_t>)(part + q * 256) = f32x4_t{c[4 * (q & 3)], c[4 * (q & 3) + 1], c[4 * (q & 3) + 2], c[4 * (q & 3) + 3]};
+      }
+    };
     if constexpr (KIND == kLossLogits) {
       auto main_loop = [&](auto iss_c) {
         using Wait = std::integral_constant<int, 2 * DLOADS>;  // the loads of this step and the last one
-        const int nk = cur.nk, units = nk / 2;
+        const int nk = cur.nk, units = nk / 2, k0 = cur.k0;
         if constexpr (decltype(iss_c)::value) LOSS_WAIT_VMCNT(4 * PL);
         __builtin_amdgcn_s_barrier();
 #pragma unroll
@@ -424,13 +448,14 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
                    if (r < MI) pf[0][r] = frag_p(an, r, 0, std::false_type{});
                    else qf[0][r - MI] = frag_w(w0, r - MI, h ? 0 : 2);
                  },
-                 [&](int i) { issue_p(i, min(k + 3, nk - 1), af, std::false_type{}); },
-                 [&](int i) { issue_w(h * PL + i, min(u + 2, units - 1), kQAt + qfar * (2 * HALF)); });
+                 [&](int i) { issue_p(i, k0 + min(k + 3, nk - 1), af, std::false_type{}); },
+                 [&](int i) { issue_w(h * PL + i, k0 / 2 + min(u + 2, units - 1), kQAt + qfar * (2 * HALF)); });
           });
           qs = qn;
         }
       };
-      if (issuer) main_loop(std::true_type{});
+      if (summed) load_sum(b.g[0].prev + part_at(b.g[0].splits));
+      else if (issuer) main_loop(std::true_type{});
       else main_loop(std::false_type{});
     } else {
       auto main_loop = [&](auto iss_c, auto trans_c) {
@@ -490,7 +515,9 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
       if (a.row_most) scale_for(a.row_most[r], inv);
       return inv * q_inv;
     };
-    if constexpr (KIND == kLossLogits) {
+    if (RANGES && a.part) {
+      store_part(a.part + part_at(a.splits) + cur.k0 / a.kper * (TB * TB));
+    } else if constexpr (KIND == kLossLogits) {
       const int c0 = cur.bj * TB + wn * 64;       // the wave's first column
       const int left = a.cols - c0;               // real columns from there
       const int wsw = swz((wm * 32 + er) & 15);
@@ -544,22 +571,29 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           a.gs[at] = s + (ones - 1.0f);
         }
         // The row's targets in this lane's columns (bits 0, 1, 3, 4, 5 of the distance from the first): found 16 at a time, then
-        // taken one by one, with their ids read again (one place in the code: a small call spends its time on fetching instructions).
-        const auto place = [&](int id) { return (id - c0) ^ (eh << 2); };
+        // taken one by one, in one place of the code (a small call spends its time on fetching instructions).
         for (int j0 = 0; j0 < a.k; j0 += 16) {
-          uint32_t hits = 0;
-          if (j0 == 0) hits = (place(id0[mi]) & ~0x3b) == 0;
+          int at[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) at[i] = -1;
+          if (j0 == 0) at[0] = id0[mi];
           if (a.k > 1) {
-            int id[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) id[i] = j0 + i < a.k ? *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j0 + i) : -1;
+            for (int i = 0; i < 16; ++i)
+              if (j0 + i < a.k) at[i] = *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j0 + i);
+          }
+          uint32_t hits = 0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) hits |= (place(id[i]) & ~0x3b) == 0 ? 1u << i : 0u;
+          for (int i = 0; i < 16; ++i) {
+            at[i] = (at[i] - c0) ^ (eh << 2);
+            hits |= (at[i] & ~0x3b) == 0 ? 1u << i : 0u;
           }
           while (hits) {
-            const int j = j0 + __builtin_ctz(hits);
+            const int i = __builtin_ctz(hits), j = j0 + i;
             hits &= hits - 1;
-            const int x = place(j == 0 ? id0[mi] : *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j));
+            int x = at[0];
+#pragma unroll
+            for (int f = 1; f < 16; ++f) x = i == f ? at[f] : x;
             const int e = (x >> 5) * 16 + ((x >> 3) & 3) * 4 + (x & 3);
             float z = 0.0f;
 #pragma unroll
@@ -629,12 +663,7 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
             for (int v = 0; v < 16; ++v) acc[i][j][v] *= f;
       }
       if (a.part) {
-#pragma unroll
-        for (int q = 0; q < MI * NI * 4; ++q) {
-          const f32x16_t& c = acc[q / (NI * 4)][(q >> 2) & 1];
-          *(gptr<f32x4_t>)(a.part + tile_at + q * 256) =
-              f32x4_t{c[4 * (q & 3)], c[4 * (q & 3) + 1], c[4 * (q & 3) + 2], c[4 * (q & 3) + 3]};
-        }
+        store_part(a.part + tile_at);
       } else if (!a.out_bf16) {
         static_for<MI>([&](auto mi_c) {
           constexpr int mi = decltype(mi_c)::value;
@@ -1290,6 +1319,13 @@ __device__ __forceinline__ void add_ranges(f32x4_t& s, const float* p, int64_t s
     if (i + e < splits) s += v[e];
 }
 
+__global__ __launch_bounds__(256) void loss_sum_kernel(float* part, int quads, int splits) {
+  float* p = part + int64_t(blockIdx.y) * splits * quads * 4 + (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  f32x4_t s = *(gptr<const f32x4_t>)p;
+  for (int i = 1; i < splits; i += 8) add_ranges(s, p, int64_t(quads) * 4, i, splits);
+  *(gptr<f32x4_t>)p = s;
+}
+
 // The K ranges' partial tiles added in order; four elements per thread.
 template <int NW, int TB>
 __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
@@ -1737,6 +1773,12 @@ hipError_t launch_loss_grad(const LossGrad& b, hipStream_t st) {
     hipLaunchKernelGGL((loss_grad_kernel<false, 2>), grid, dim3(256), 0, st, a);
   else
     hipLaunchKernelGGL((loss_grad_kernel<false, 1>), grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_sum(float* part, int64_t tiles, int tile, int splits, hipStream_t st) {
+  const int quads = tile * tile / 4;
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(unsigned(quads / 256), unsigned(tiles)), dim3(256), 0, st, part, quads, splits);
   return hipGetLastError();
 }
 

@@ -6,6 +6,7 @@
 //     prep    the labels in one form (first chunk); x's rows panel blocked; a copy of w where it cannot be read as
 //             it lies (first chunk)
 //     logits  z = x w^T: per row and 64 columns the softmax partials, the targets' logits and (for gradients) the logits
+//             (few tiles of a long K: the K ranges' sums, their total, and from it the rest: three launches)
 //     rows    the partials joined: the tokens' losses, and the weights of their gradients; with MEAN (first chunk) the weights'
 //             sum
 //     grad    dz in the logits' place; (last chunk) the loss
@@ -98,15 +99,29 @@ Gemm grid_of(int tile, int64_t M, int64_t N) {
   g.tn = int(up(N, tile) / tile);
   return g;
 }
-// The tile of a product that runs alone.
-Gemm choose(int64_t M, int64_t N, int64_t steps) {
-  Gemm g[2] = {grid_of(kLossTile, M, N), grid_of(kLossTileSmall, M, N)};
-  double us[2];
-  for (int i = 0; i < 2; ++i) {
-    const int64_t items = g[i].items();
-    us[i] = launch_us(g[i].tile, 1, &items, &steps);
+// The tile of a product that runs alone; its K ranges if it may have them (the logits: on 128 x 128 tiles, in one round and of an even
+// number of steps, at least 16, each; their sum and the epilogue, launches of their own, taken as 14 us and the sum's traffic. 553 tokens, 722 ids, 1088 wide, fp32:
+// 35 us, 43 in one range; 300 tokens, 400 ids, 4000 wide: 28 and 117 us).
+Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
+  Gemm best;
+  double us = 0.0;
+  for (int tile : {kLossTile, kLossTileSmall}) {
+    Gemm g = grid_of(tile, M, N);
+    const int64_t tiles = g.items(), most = ranges && tile == kLossTileSmall ? std::min<int64_t>(512 / tiles, steps / 16) : 1;
+    for (int64_t s = 1; s == 1 || s <= most; ++s) {
+      const int64_t kper = s == 1 ? steps : up((steps + s - 1) / s, 2), items = tiles * s;
+      if (s > 1 && (steps + kper - 1) / kper != s) continue;
+      double t = launch_us(tile, 1, &items, &kper);
+      if (s > 1) t += 14.0 + double(items) * tile * tile * 8.0 / 4.9e6;
+      if (best.tile == 0 || t < us) {
+        us = t;
+        best = g;
+        best.splits = int(s);
+        best.kper = int(kper);
+      }
+    }
   }
-  return g[us[1] < us[0]];
+  return best;
 }
 // The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K; 0: not asked for) in one launch, and the K ranges of dx: each range
 // at least 16 steps long, the join of the ranges taken as its traffic and a launch.
@@ -197,8 +212,9 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
       part = size_t(p.dx.splits) * size_t(p.chunk * p.hp) * 4;
     }
   } else {
-    p.logits = choose(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.nseg * p.hk / 32);
+    p.logits = choose(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.nseg * p.hk / 32, true);
     p.logits.nk = int(p.hk / 32);
+    if (p.logits.splits > 1) part = size_t(p.logits.items()) * size_t(p.logits.tile) * p.logits.tile * 4;
   }
   const int64_t wsteps = p.out_nseg * up(std::min(p.chunk, std::max<int64_t>(p.n, 1)), 32) / 32;
   if (a->dx && !p.stream) {
@@ -210,7 +226,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
     for (const Gemm& g : {p.dx, alone})
       if (g.splits > 1) part = std::max(part, size_t(g.items()) * size_t(g.tile) * g.tile * 4);
   } else if (a->dw) {
-    p.dw = choose(p.v, p.h, wsteps);
+    p.dw = choose(p.v, p.h, wsteps, false);
   }
   size_t o = 0;
   auto take = [&](int64_t bytes) {
@@ -398,7 +414,14 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       z.ldc = p.vp;
       if (p.grads && p.f32) z.logits = f32p(p.z32);
       if (p.grads && !p.f32) z.codes = u16p(p.codes);
+      if (z.splits > 1) z.part = f32p(p.part);
       LOSS_TRY(launch_loss_gemm(zz, kLossLogits, p.logits.tile, st), "logits launch");
+      if (z.splits > 1) {
+        LOSS_TRY(launch_loss_sum(z.part, int64_t(z.tm) * z.tn, p.logits.tile, z.splits, st), "logits sum launch");
+        z.prev = z.part;
+        z.part = nullptr;
+        LOSS_TRY(launch_loss_gemm(zz, kLossLogits, p.logits.tile, st), "logits epilogue launch");
+      }
     }
 
     LossRows rw{};

@@ -61,7 +61,9 @@ struct LossGemm {
   uint16_t* codes;                                 // 16-bit logits, panel blocked with ldc columns, or null
   float* logits;                                   // fp32 logits, row-major with ldc columns, or null
   int64_t ldc;
-  // gradients: the result, row-major with ldo columns, or fp32 tiles in accumulator order (part); prev: such tiles to add
+  // gradients: the result, row-major with ldo columns, or fp32 tiles in accumulator order (part); prev: such tiles to add.
+  // logits: part: the sums of a K range, in such tiles, and nothing else; prev: tiles with the sum over the ranges, `splits` tiles apart,
+  // instead of a product
   void* out;
   int64_t ldo;
   int32_t out_bf16;
@@ -225,6 +227,8 @@ inline int loss_row_blocks(const LossRows& a) { return a.gstep == 1 ? a.rows_pad
 hipError_t launch_loss_total(const LossTotal& a, hipStream_t st);
 hipError_t launch_loss_grad(const LossGrad& a, hipStream_t st);
 hipError_t launch_loss_join(const LossJoin& a, int tile, hipStream_t st);
+// logits in K ranges: the ranges of each tile added in order, into the first one's place
+hipError_t launch_loss_sum(float* part, int64_t tiles, int tile, int splits, hipStream_t st);
 hipError_t launch_loss_zero(void* p, int64_t bytes, hipStream_t st);
 hipError_t launch_scale_grad(void* p, int64_t n, int bf16, const float* factor, hipStream_t st);
 

@@ -181,6 +181,31 @@ def test_distill_matches_the_oracle(n, v, h, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,v,h,chunk", [(9, 500, 4000, 0), (200, 700, 2100, 0), (300, 130, 3001, 256), (1, 60, 4096, 0)])
+def test_long_rows_of_few_tiles(n, v, h, chunk, dtype):
+    """The logits' products are cut into K ranges."""
+    rng = np.random.default_rng(29)
+    x, w, x64, w64 = _inputs(rng, n, v, h, dtype)
+    t = _labels(rng, n, v, 0.2 if n > 1 else 0.0)
+    _say(n, v, h, chunk, dtype)
+    ref = _Ref(OL.linear_xent(x64, w64, t), t >= 0, None, "mean", 1.0)
+    q = np.zeros((n, v), bool)
+    q[np.nonzero(t >= 0)[0], t[t >= 0]] = True
+    got = _call("xent", x, w, dtype, t, chunk_rows=chunk)
+    _check(got, ref, x64, w64, dtype, q, what=f"long rows {n}x{v}x{h} {dtype}")
+    _check_loss(got, ref)
+    only = _call("xent", x, w, dtype, t, outs=("loss", "token_loss", "lse"), chunk_rows=chunk)
+    for o in only:
+        np.testing.assert_array_equal(only[o], got[o])
+    ids, lg = _teacher(rng, n, v, 20, empty=0.1 if n > 1 else 0.0)
+    got = _call("distill", x, w, dtype, (ids, lg, F32), temperature=2.0)
+    ref = _Ref(OL.linear_distill(x64, w64, ids, lg, temperature=2.0), (ids >= 0).any(1), None, "mean", 1.0)
+    q[:] = False
+    q[np.repeat(np.arange(n), 20).reshape(n, 20)[ids >= 0], ids[ids >= 0]] = True
+    _check(got, ref, x64, w64, dtype, q, inv_t=0.5, what=f"distill long rows {n}x{v}x{h} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_chunks_of_rows_add_up(dtype):
     """Three passes over the rows, the last one ragged: dw is summed in fp32 across them."""
     rng = np.random.default_rng(21)
