@@ -423,7 +423,10 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  *                outputs has to be given)
  *   chunk_rows   0, or the most rows of x per pass where gradients are asked for (rounded up to 256): fewer rows take
  *                less workspace and more time. 0: as many as fit 2 GiB of 16-bit logits.
- * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0.
+ * No output may overlap an input or another output.
+ * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0. The other rows
+ * and w have to be finite: an infinity or a NaN there may make any result NaN. A BF16 logit that overflows to -inf is a
+ * probability of 0.
  * Precision: bf16 products have fp32 accumulation; the softmax is formed in fp32, the sum of a row without its largest
  * term, so that the loss of a token that the model is sure of keeps its digits; the logits' gradient is rounded to bf16
  * before its two products, and each result once to bf16. F32: products at fp32 accuracy (two scaled fp16 parts per operand:

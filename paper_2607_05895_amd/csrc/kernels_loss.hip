@@ -553,13 +553,14 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         float m = u[0];
 #pragma unroll
         for (int e = 1; e < 32; ++e) m = fmaxf(m, u[e]);
-        m = top[mi] = half_max(m);
+        m = half_max(m);
+        const float ref = top[mi] = fmaxf(m, -3.4e38f);  // (64 logits of -inf: terms of 0)
         // Sum of the others' exp: the largest term itself is 1, and what is far below it must not vanish in that 1. A
         // term's fraction is the term, but 0 for a 1; how many ones there are (equal logits) is what the two sums differ by.
         float s = 0.0f, all = 0.0f;
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-          const float x = __builtin_amdgcn_exp2f((u[e] - m) * L);
+          const float x = __builtin_amdgcn_exp2f((u[e] - ref) * L);
           s += __builtin_amdgcn_fractf(x);
           all += x;
         }
@@ -1499,10 +1500,11 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
 #pragma unroll
           for (int e = 1; e < 16; ++e) m = fmaxf(m, u[e]);
           m = half_max(m);
+          const float ref = fmaxf(m, -3.4e38f);
           float s = 0.0f, all = 0.0f;  // as in loss_gemm_kernel
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float x = __builtin_amdgcn_exp2f((u[e] - m) * L);
+            const float x = __builtin_amdgcn_exp2f((u[e] - ref) * L);
             s += __builtin_amdgcn_fractf(x);
             all += x;
           }
@@ -1528,7 +1530,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
               *(gptr<u32x2>)(a.codes + blk_index(row, c0 + g * 8 + fh * 4, a.ldc)) =
-                  u32x2{code2((u[4 * g] - m) * C, (u[4 * g + 1] - m) * C), code2((u[4 * g + 2] - m) * C, (u[4 * g + 3] - m) * C)};
+                  u32x2{code2((u[4 * g] - ref) * C, (u[4 * g + 1] - ref) * C), code2((u[4 * g + 2] - ref) * C, (u[4 * g + 3] - ref) * C)};
           }
         });
       }

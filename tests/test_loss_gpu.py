@@ -382,6 +382,44 @@ def test_large_logits_do_not_overflow(size, dtype):
     assert np.isfinite(got["dx"]).all() and np.isfinite(got["dw"]).all()
 
 
+@pytest.mark.parametrize("n,v,h", [(5, 400, 32), (300, 400, 32), (5, 4400, 32), (100, 4400, 32)])
+def test_ids_of_minus_infinity_have_no_share(n, v, h):
+    """128 ids and more in a row, whole softmax partials among them, whose logit overflows to -inf for every token."""
+    rng = np.random.default_rng(30)
+    x, w, x64, w64 = _inputs(rng, n, v, h, BF16)
+    x[:, 0], x64[:, 0] = 0x4000, 2.0
+    off = np.zeros(v, bool)
+    off[60:200] = off[v - 3:] = True
+    w[off] = 0
+    w[off, 0] = 0xFF7F  # -3.4e38
+    t = rng.choice(np.nonzero(~off)[0], n)
+    _say(n, v, h)
+    got = _call("xent", x, w, BF16, t)
+    ref = _Ref(OL.linear_xent(x64, w64[~off], np.cumsum(~off)[t] - 1), np.ones(n, bool), None, "mean", 1.0)
+    assert not got["dw"][off].any()
+    got["dw"] = got["dw"][~off]
+    q = np.zeros((n, int((~off).sum())), bool)
+    q[np.arange(n), np.cumsum(~off)[t] - 1] = True
+    _check(got, ref, x64, w64[~off], BF16, q, what=f"-inf {n}x{v}x{h}")
+    _check_loss(got, ref)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_tokens_than_one_pass_takes(dtype):
+    """65536 rows and a ragged second pass."""
+    rng = np.random.default_rng(31)
+    n, v, h = 66001, 90, 24
+    x, w, x64, w64 = _inputs(rng, n, v, h, dtype)
+    t = _labels(rng, n, v)
+    _say(n, v, h, dtype)
+    got = _call("xent", x, w, dtype, t, reduction="sum")
+    ref = _Ref(OL.linear_xent(x64, w64, t, reduction="sum"), t >= 0, None, "sum", 1.0)
+    q = np.zeros((n, v), bool)
+    q[np.nonzero(t >= 0)[0], t[t >= 0]] = True
+    _check(got, ref, x64, w64, dtype, q, what=f"{n}x{v}x{h} {dtype}")
+    _check_loss(got, ref)
+
+
 def test_equal_logits():
     """Every logit equal (a head of equal rows): loss log v, whatever the size of the logits."""
     import torch
