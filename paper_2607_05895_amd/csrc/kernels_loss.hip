@@ -22,6 +22,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
 using gptr = __attribute__((address_space(1))) T*;
 template <typename T>
@@ -547,6 +549,15 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         constexpr int mi = decltype(mi_c)::value;
         const int row = row0 + mi * 32;
         const float inv_t = inv_ts[mi], L = kLog2e * inv_t;
+        // the row's first 16 targets, on their way during the softmax (past the last one lie the next row's, or the workspace's next array)
+        i32x4 at[4] = {};
+        auto load_ids = [&](int j0) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (j0 + v * 4 < a.k) at[v] = *(gptr<const i32x4_a4>)(a.ids + int64_t(row) * a.k + j0 + v * 4);
+        };
+        if (a.k > 1) load_ids(0);
+        else at[0][0] = id0[mi];
         float u[32];  // logits before the temperature
 #pragma unroll
         for (int e = 0; e < 32; ++e) u[e] = acc[mi][e >> 4][e & 15];
@@ -571,30 +582,28 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           a.gm[at] = m * inv_t;
           a.gs[at] = s + (ones - 1.0f);
         }
-        // The row's targets in this lane's columns (bits 0, 1, 3, 4, 5 of the distance from the first): found 16 at a time, then
-        // taken one by one, in one place of the code (a small call spends its time on fetching instructions).
+        // the row's targets among the wave's columns, 16 at a time, then one by one, in one place of the code (a small call spends its
+        // time on fetching instructions)
         for (int j0 = 0; j0 < a.k; j0 += 16) {
-          int at[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) at[i] = -1;
-          if (j0 == 0) at[0] = id0[mi];
-          if (a.k > 1) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (j0 + i < a.k) at[i] = *(gptr<const int32_t>)(a.ids + int64_t(row) * a.k + j0 + i);
-          }
+          if (j0 > 0) load_ids(j0);
           uint32_t hits = 0;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            at[i] = (at[i] - c0) ^ (eh << 2);
-            hits |= (at[i] & ~0x3b) == 0 ? 1u << i : 0u;
-          }
+          for (int v = 0; v < 4; ++v)
+            if (v == 0 || j0 + v * 4 < a.k) {
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                at[v][t] -= c0;
+                hits |= uint32_t(at[v][t]) < 64u ? 1u << (v * 4 + t) : 0u;
+              }
+            }
+          if (a.k - j0 < 16) hits &= (1u << (a.k - j0)) - 1;
           while (hits) {
             const int i = __builtin_ctz(hits), j = j0 + i;
             hits &= hits - 1;
-            int x = at[0];
+            int x = at[0][0];
 #pragma unroll
-            for (int f = 1; f < 16; ++f) x = i == f ? at[f] : x;
+            for (int f = 1; f < 16; ++f) x = i == f ? at[f >> 2][f & 3] : x;
+            if (((x >> 2) & 1) != eh) continue;  // (the other half wave's column)
             const int e = (x >> 5) * 16 + ((x >> 3) & 3) * 4 + (x & 3);
             float z = 0.0f;
 #pragma unroll
@@ -1515,14 +1524,35 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
             a.gm[at] = m * a.inv_t;
             a.gs[at] = s + (ones - 1.0f);
           }
-          for (int j = 0; j < a.k; ++j) {
-            const int x = (a.ids[row * a.k + j] - c0) ^ (fh << 2);
-            if ((x & ~0x1b) == 0) {
+          // targets, as in loss_gemm_kernel, among 32 columns
+          for (int j0 = 0; j0 < a.k; j0 += 16) {
+            i32x4 at[4] = {};
+            if (a.k == 1) {
+              at[0][0] = a.ids[row];
+            } else {
+#pragma unroll
+              for (int v = 0; v < 4; ++v)
+                if (j0 + v * 4 < a.k) at[v] = *(gptr<const i32x4_a4>)(a.ids + row * a.k + j0 + v * 4);
+            }
+            uint32_t hits = 0;
+#pragma unroll
+            for (int f = 0; f < 16; ++f) {
+              at[f >> 2][f & 3] -= c0;
+              hits |= uint32_t(at[f >> 2][f & 3]) < 32u ? 1u << f : 0u;
+            }
+            if (a.k - j0 < 16) hits &= (1u << (a.k - j0)) - 1;
+            while (hits) {
+              const int i = __builtin_ctz(hits);
+              hits &= hits - 1;
+              int x = at[0][0];
+#pragma unroll
+              for (int f = 1; f < 16; ++f) x = i == f ? at[f >> 2][f & 3] : x;
+              if (((x >> 2) & 1) != fh) continue;
               const int e = ((x >> 3) & 3) * 4 + (x & 3);
               float z = 0.0f;
 #pragma unroll
               for (int f = 0; f < 16; ++f) z = e == f ? u[f] : z;
-              a.zt[row * a.k + j] = z * a.inv_t;
+              a.zt[row * a.k + j0 + i] = z * a.inv_t;
             }
           }
           if (a.codes) {
