@@ -413,7 +413,7 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
 
 /* n tokens with hidden states x through an output head w: logits z = x w^T (n x v), which are never held as a whole (a
  * chunk of rows at 16 bits each where gradients are asked for, none otherwise).
- *   x, w         n x h and v x h of dtype (F32 or BF16), read only; 0 <= n <= 2^28, 1 <= v, h <= 2^20
+ *   x, w         n x h and v x h of dtype (F32 or BF16), read only; 0 <= n <= 2^25, 1 <= v, h <= 2^20
  *   reduction, scale  an mfsdp_reduction and a finite factor; the gradients are those of loss
  *   token_weight optional n fp32 weights a_r (NULL: 1)
  *   loss         optional, 1 fp32: the reduced loss
@@ -429,7 +429,7 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  * probability of 0.
  * Precision: bf16 products have fp32 accumulation; the softmax is formed in fp32, the sum of a row without its largest
  * term, so that the loss of a token that the model is sure of keeps its digits; the logits' gradient is rounded to bf16
- * before its two products, and each result once to bf16. F32: products at fp32 accuracy (two scaled fp16 parts per operand:
+ * before its two products (up to 128 tokens it is held to 16 bits and more), and each result once to bf16. F32: products at fp32 accuracy (two scaled fp16 parts per operand:
  * a value of w is off by at most 2^-24 of itself or 2^-40 of w's largest, an element of a row of x or of the logits' gradient by as
  * much relative to its row), everything else in fp32. */
 typedef struct {

@@ -33,7 +33,7 @@ namespace {
 
 static_assert(MFSDP_MAX_TOP_LOGITS == kLossMaxTop, "teacher logits of the ABI and the kernel");
 
-constexpr int64_t kMaxTokens = int64_t(1) << 28;
+constexpr int64_t kMaxTokens = int64_t(1) << 25;  // (a launch holds fewer than 2^32 threads, the labels take 64 a token)
 constexpr int64_t kMaxSide = int64_t(1) << 20;
 constexpr int64_t kMaxChunk = 65536;
 constexpr int64_t kLogitBytes = int64_t(1) << 31;  // of a chunk's logits, at 16 bits each
@@ -149,7 +149,7 @@ void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wstep
 
 int check(const mfsdp_head_loss* a, int64_t k, bool pointers) {
   if (!a) return fail(MFSDP_E_INVALID, "arguments are NULL");
-  if (a->n < 0 || a->n > kMaxTokens) return fail(MFSDP_E_INVALID, "n must be in [0, 2^28]");
+  if (a->n < 0 || a->n > kMaxTokens) return fail(MFSDP_E_INVALID, "n must be in [0, 2^25]");
   if (a->v < 1 || a->v > kMaxSide) return fail(MFSDP_E_INVALID, "v must be in [1, 2^20]");
   if (a->h < 1 || a->h > kMaxSide) return fail(MFSDP_E_INVALID, "h must be in [1, 2^20]");
   if (k < 1 || k > kLossMaxTop) return fail(MFSDP_E_INVALID, "k must be in [1, MFSDP_MAX_TOP_LOGITS]");

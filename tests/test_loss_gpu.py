@@ -405,6 +405,21 @@ def test_ids_of_minus_infinity_have_no_share(n, v, h):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,v,h", [(3, 1 << 20, 8), (2, 300, 1 << 16)])
+def test_longest_sides(n, v, h, dtype):
+    rng = np.random.default_rng(33)
+    x, w, x64, w64 = _inputs(rng, n, v, h, dtype)
+    t = np.array([v - 1, 0, v // 2])[:n]
+    _say(n, v, h, dtype)
+    got = _call("xent", x, w, dtype, t)
+    ref = _Ref(OL.linear_xent(x64, w64, t), t >= 0, None, "mean", 1.0)
+    q = np.zeros((n, v), bool)
+    q[np.arange(n), t] = True
+    _check(got, ref, x64, w64, dtype, q, what=f"{n}x{v}x{h} {dtype}")
+    _check_loss(got, ref)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_more_tokens_than_one_pass_takes(dtype):
     """65536 rows and a ragged second pass."""
     rng = np.random.default_rng(31)
@@ -543,6 +558,64 @@ def test_repeated_calls_streams_and_replays_give_the_same_bits():
         assert all(torch.equal(p, q) for p, q in zip(want, _bits(e + f))), i
         both(a, b, xd2, ws)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n,v,h,k,dtype", [(40, 5000, 136, 1, BF16), (128, 4200, 72, 6, BF16), (300, 1500, 136, 7, F32),
+                                           (16, 700, 2112, 1, F32), (2048, 20000, 256, 1, BF16)])
+def test_two_calls_at_once_and_replays(n, v, h, k, dtype):
+    """Two streams with a workspace each, side by side; then two captured calls, replayed with eager work in between: the bits of
+    a call alone."""
+    import torch
+    rng = np.random.default_rng(32)
+    w = to_dev(_inputs(rng, 1, v, h, dtype)[1], dtype)
+    xs = [to_dev(_inputs(rng, n, 1, h, dtype)[0], dtype) for _ in range(2)]
+    t = torch.from_numpy(_labels(rng, n, v)).cuda()
+    ids, lg = (torch.from_numpy(a).cuda() for a in _teacher(rng, n, v, k))
+    _say(n, v, h, k, dtype)
+
+    def outs():
+        return [torch.zeros(1, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros_like(xs[0]), torch.zeros_like(w)]
+
+    def call(x, o, ws):
+        kw = dict(loss=o[0], token_loss=o[1], dx=o[2], dw=o[3], workspace=ws)
+        if k == 1:
+            native.linear_xent_t(x, w, t, **kw)
+        else:
+            native.linear_distill_t(x, w, ids, lg, **kw)
+
+    args = native.head_loss_args_t(xs[0], w, dx=xs[0], dw=w)
+    wss = [native.head_loss_workspace_t(args, k) for _ in range(2)]
+    want = []
+    for x in xs:
+        o = outs()
+        call(x, o, wss[0])
+        want.append(_bits(o))
+
+    def same(got):
+        torch.cuda.synchronize()
+        for o, bits in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(_bits(o), bits))
+            for a in o:
+                a.zero_()
+
+    got, streams = [outs(), outs()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                call(xs[i], got[i], wss[i])
+    same(got)
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(xs[i], got[i], wss[i])
+        graphs.append(g)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+        same(got)
+        call(xs[1], got[0], wss[0])
 
 
 def test_helpers_refuse_what_does_not_fit():
