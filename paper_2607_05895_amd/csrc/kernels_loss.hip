@@ -49,9 +49,9 @@ __device__ __forceinline__ int swz(int r) { return ((r >> 1 ^ r >> 3) & 1) | (((
 #define LOSS_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 0xF) | (((n) >> 4) << 14) | (7 << 4) | (0xF << 8))
 #define LOSS_WAIT_LGKM0() __builtin_amdgcn_s_waitcnt(0xF | (7 << 4) | (0 << 8) | (3 << 14))
 
-// A transposing read (four rows by one column per lane and 16 lanes). Through a restrict pointer: without alias information of
-// their own the compiler takes these reads to depend on every load into LDS in flight and waits for all of them
-// (8192 x 4096 x 128256: 0.99 PFLOP/s so, 1.47 without those waits, as with plain reads of a transposed copy).
+// A transposing read (four rows by one column per lane and 16 lanes). Through a restrict pointer: without alias information
+// of their own the compiler takes these reads to depend on every load into LDS in flight and waits for all of them (8192 x
+// 4096 x 128256: 0.99 PFLOP/s so, 1.47 without those waits, as with plain reads of a transposed copy).
 __device__ __forceinline__ bf16x4_t read_tr(lptr<bf16x4_t> __restrict p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(p);
 }
@@ -140,9 +140,9 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   const int per = min(G::SLOTS, (total + kGemmXcds - 1) / kGemmXcds);  // items of one group
   const int groups = (total + per - 1) / per;
 
-  // Items are dealt in groups that run together on one XCD: group g belongs to XCD g % 8. A workgroup's first item is its place in
-  // its XCD's first group; the next ones come from a counter of its XCD or, once that has run out, of the XCD with the
-  // most items left. (One lane asks; -1: none left.)
+  // Items are dealt in groups that run together on one XCD: group g belongs to XCD g % 8. A workgroup's first item is its
+  // place in its XCD's first group; the next ones come from a counter of its XCD or, once that has run out, of the XCD with
+  // the most items left. (One lane asks; -1: none left.)
   const int home = blockIdx.x % kGemmXcds, place = blockIdx.x / kGemmXcds;
   if (place >= per) return;
   auto left_in = [&](int x, int taken) {  // XCD x's items beyond its first group that are not taken yet
@@ -189,10 +189,10 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   };
 
   const bool issuer = w < DW;
-  // Lane offsets (bytes) of a load: a 1 KiB block (lane l: row l / 4, 16-byte chunk (l % 4) ^ swz(row), so that the plain fragment
-  // reads are conflict-free); eight 128-byte lines of w (row l / 8, chunk (l % 8) ^ (row / 2) % 8); 64 lanes along TB columns of
-  // w's rows (chunk ^ 4 (row % 4)). Loads past w's last 16 bytes are held there: what they bring meets zeros of x or dz, or
-  // belongs to columns that are not stored.
+  // Lane offsets (bytes) of a load: a 1 KiB block (lane l: row l / 4, 16-byte chunk (l % 4) ^ swz(row), so that the plain
+  // fragment reads are conflict-free); eight 128-byte lines of w (row l / 8, chunk (l % 8) ^ (row / 2) % 8); 64 lanes along
+  // TB columns of w's rows (chunk ^ 4 (row % 4)). Loads past w's last 16 bytes are held there: what they bring meets zeros of
+  // x or dz, or belongs to columns that are not stored.
   const uint32_t loff = (lane >> 2) * kRowB + ((lane & 3) ^ swz(lane >> 2)) * 16;
   constexpr int RPL = 512 / TB;  // rows of w per load of TB columns
   // of the tile whose loads are being issued
@@ -234,7 +234,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
                                              (lds_byte*)(smem + at), 16, voff, soff, 0, 0);
   };
   // Step k of all segments: the step in its segment, and the bytes to its parts of P and Q. fp32 operands lie in two fp16
-  // parts (F16), few tokens' dz in two bf16 parts; the pairs (1, 0), (0, 1) (F16), (0, 0): the small products first, while the sum is small.
+  // parts (F16), few tokens' dz in two bf16 parts; the pairs (1, 0), (0, 1) (F16), (0, 0): the small products first, while
+  // the sum is small.
   auto in_segment = [&](int k, int64_t& po, int64_t& qo) {
     po = qo = 0;
     if constexpr (NSEG > 1) {
@@ -245,8 +246,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     }
     return k;
   };
-  // load i (of PL) of step k of P, of Q, into `at`. A blocked operand's next step is one block further along each panel, or (read
-  // transposed) two panels further down; load i moves block i DW + w of the step.
+  // load i (of PL) of step k of P, of Q, into `at`. A blocked operand's next step is one block further along each panel, or
+  // (read transposed) two panels further down; load i moves block i DW + w of the step.
   auto issue_blocked = [&](const char* base, uint32_t row32, int i, int at, auto trans_c) {
     const int blk = i * DW + w;
     if constexpr (decltype(trans_c)::value)
@@ -309,8 +310,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
     }
   };
 
-  // Fragment addresses: plain (row lane % 32 of a block of 32, chunk 2 slice + lane / 32) and transposed (lane: rows lane / 4 % 4
-  // (+ 4) + 8 (lane / 32), columns 4 (lane % 4) + 16 (lane / 16 % 2) of 32).
+  // Fragment addresses: plain (row lane % 32 of a block of 32, chunk 2 slice + lane / 32) and transposed (lane: rows lane / 4
+  // % 4 (+ 4) + 8 (lane / 32), columns 4 (lane % 4) + 16 (lane / 16 % 2) of 32).
   const int frow = lane & 31, fhalf = lane >> 5;
   const int prow = (wm * (MI * 32) + frow) * kRowB, slot0 = ((0 + fhalf) ^ swz(frow)) * 16, slot1 = ((2 + fhalf) ^ swz(frow)) * 16;
   const int trow = (lane >> 5) * 8 + ((lane >> 2) & 3), tchunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1), tbyte = (lane & 1) * 8;
@@ -347,7 +348,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
   Item cur, nxt;
   if (!item_at(home * per + place, cur)) return;
   if (issuer && !summed) prologue(cur);
-  // (the last part of LDS is free whenever items are taken; the last wave asks: of eight waves it issues no loads to wait behind)
+  // (the last part of LDS is free whenever items are taken; the last wave asks: of eight waves it issues no loads to wait
+  // behind)
   int* mail = reinterpret_cast<int*>(smem + kSlabAt);
   const bool asks = threadIdx.x == (NW - 1) * 64, queued = groups > kGemmXcds;
   bool has_next = false;
@@ -376,7 +378,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[sl][j], pf[sl][i], acc[i][j], 0, 0, 0);
     };
     // One step: the first slice with the second one's reads and P's loads; half of the second slice with Q's loads; the
-    // barrier; the rest with the next step's first reads. wait_c: loads that may still be in flight for the next step to have landed.
+    // barrier; the rest with the next step's first reads. wait_c: loads that may still be in flight for the next step to have
+    // landed.
     auto step = [&](auto iss_c, auto wait_c, auto read1, auto read0, auto load_p, auto load_q) {
       constexpr bool ISS = decltype(iss_c)::value;
       __builtin_amdgcn_sched_barrier(0);
@@ -549,7 +552,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
         constexpr int mi = decltype(mi_c)::value;
         const int row = row0 + mi * 32;
         const float inv_t = inv_ts[mi], L = kLog2e * inv_t;
-        // the row's first 16 targets, on their way during the softmax (past the last one lie the next row's, or the workspace's next array)
+        // the row's first 16 targets, on their way during the softmax (past the last one lie the next row's, or the
+        // workspace's next array)
         i32x4 at[4] = {};
         auto load_ids = [&](int j0) {
 #pragma unroll
@@ -582,8 +586,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           a.gm[at] = m * inv_t;
           a.gs[at] = s + (ones - 1.0f);
         }
-        // the row's targets among the wave's columns, 16 at a time, then one by one, in one place of the code (a small call spends its
-        // time on fetching instructions)
+        // the row's targets among the wave's columns, 16 at a time, then one by one, in one place of the code (a small call
+        // spends its time on fetching instructions)
         for (int j0 = 0; j0 < a.k; j0 += 16) {
           if (j0 > 0) load_ids(j0);
           uint32_t hits = 0;
@@ -696,8 +700,8 @@ __global__ __launch_bounds__(NW * 64, TB == kLossTile ? 1 : 2) void loss_gemm_ke
           }
         });
       } else {
-        // bf16, row-major, through the free stage: each wave its own 32 rows of 128 bytes at a time, whole lines per store, and
-        // no wave waits for another; 16-byte slots XORed by the row
+        // bf16, row-major, through the free stage: each wave its own 32 rows of 128 bytes at a time, whole lines per store,
+        // and no wave waits for another; 16-byte slots XORed by the row
         const int slab_w = w * 4096;
         auto at = [](int r, int s) { return r * 128 + ((s ^ r) & 7) * 16; };
         static_for<MI>([&](auto mi_c) {
@@ -1042,14 +1046,15 @@ __device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float
   m = hi;
 }
 
-// (p - q) (1 + s) of a target with weight q whose logit is d above the row's largest and e = exp(d): from what is exact where p and q are near 1
+// (p - q) (1 + s) of a target with weight q whose logit is d above the row's largest and e = exp(d): from what is exact where
+// p and q are near 1
 __device__ __forceinline__ float target_pq(float q, float d, float e, float s) {
   return e >= 0.5f && q >= 0.5f ? expm1f(d) + (1.0f - q) - q * s : e - q * (1.0f + s);
 }
 
-// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB. Many tokens: 32 rows,
-// whose partials of a group lie together. Few: one row, whose partials lie in one piece (128256 ids, 48 tokens: 7 us; with four
-// rows each and the other layout 19.5, when a workgroup reads four times the bytes it needs).
+// RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB. Many tokens: 32
+// rows, whose partials of a group lie together. Few: one row, whose partials lie in one piece (128256 ids, 48 tokens: 7 us;
+// with four rows each and the other layout 19.5, when a workgroup reads four times the bytes it needs).
 template <int RPB>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
   constexpr int GS = 1024 / RPB, BATCH = 8;
@@ -1107,7 +1112,8 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
       m = sm[0][rl];
       s = ss[0][rl];
     }
-    // sum of q (m - z) over the row's targets; a bound on |dz| at them, in units of 1 / (1 + s); whether one of them is the largest
+    // sum of q (m - z) over the row's targets; a bound on |dz| at them, in units of 1 / (1 + s); whether one of them is the
+    // largest
     const float top = m, others = s;
     const float lz = 2.0f * a.z_loss * (top + log1pf(others));
     float d = 0.0f, bound = 0.0f;
@@ -1356,9 +1362,10 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
 
 // Products for at most 32 MI tokens (LossStream). Eight waves; K in steps through a ring of NST stages filled NST - 1 steps
 // ahead by direct loads. Bound by HBM: w is read once, QB bytes per step, with up to (NST - 1) steps of it in flight per CU.
-// logits: a stage holds QR rows of w by KT of h; a wave takes all tokens by 32 rows of w, and half of the step's K where QR = 128
-//   (the halves are added in LDS at the tile's end). 128 rows of 256 bytes rather than 256 of 128: a head of 128256 x 4096 is read
-//   in 215 us (4.9 TB/s) instead of 227; more tokens leave no room for it.
+// logits: a stage holds QR rows of w by KT of h; a wave takes all tokens by 32 rows of w, and half of the step's K where
+//   QR = 128 (the halves are added in LDS at the tile's end); chunk c of row r in slot c ^ r % 16 (KT = 64: c ^ r / 2 % 8). 128
+//   rows of 256 bytes rather than 256 of 128: a head of 128256 x 4096 is read in 215 us (4.9 TB/s) instead of 227; more
+//   tokens leave no room for it.
 // dx: KT rows of w by 256 of h, a wave 32 columns; chunk c of row r in slot c ^ 2 (r % 4); fragments read transposed.
 // Past a row's end lie the next row's values, past w's end its last ones: they meet zeros of x or dz, or belong to columns
 // that are not stored.
@@ -1578,10 +1585,11 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
   LOSS_WAIT_VMCNT(0);
 }
 
-// dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). A workgroup of four waves keeps CT columns
-// of x in registers and goes through blocks of 64 rows (ids), gridDim.y blocks apart: both parts of the next block of dz are on
-// their way while this one's product goes out, through LDS, so that a wave stores whole rows of CT columns. (48 tokens, 128256 x 4096,
-// 1.05 GB: DW48 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel more.)
+// dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). A workgroup of four waves keeps CT
+// columns of x in registers and goes through blocks of 64 rows (ids), gridDim.y blocks apart: both parts of the next block of
+// dz are on their way while this one's product goes out, through LDS, so that a wave stores whole rows of CT columns. (48
+// tokens, 128256 x 4096, 1.05 GB: 245 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel
+// more.)
 template <int KS>
 __global__ __launch_bounds__(256) void loss_dw_kernel(const LossGemm a) {
   constexpr int NPAN = 2 * KS, NJ = KS <= 2 ? 2 : 1, CT = 128 * NJ, CB = CT / 32;  // panels of 16 tokens; columns, in blocks of 32

@@ -73,9 +73,9 @@ constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
 
 // A launch's time in us on `tile` x `tile` tiles, items[i] of steps[i] K steps each: what the chip's workgroups share, or the
 // longest item if that is more, and half of the shortest kind for the uneven end. Measured: a step of 32 takes 0.74 us on a
-// 256 x 256 tile (1.45 PFLOP/s over 256 CUs) and a tile's start and epilogue 8 us; on 128 x 128 tiles 0.3 and 5 us with a CU of their
-// own, 0.55 and 13 us on two that share one (4096 tokens, 20000 x 4096 head, dx and dw: 1064 us on 256 x 256 tiles, 1433 on
-// 128 x 128; 200 tokens, 2000 x 2048: 30 and 23 us).
+// 256 x 256 tile (1.45 PFLOP/s over 256 CUs) and a tile's start and epilogue 8 us; on 128 x 128 tiles 0.3 and 5 us with a CU
+// of their own, 0.55 and 13 us on two that share one (4096 tokens, 20000 x 4096 head, dx and dw: 1064 us on 256 x 256 tiles,
+// 1433 on 128 x 128; 200 tokens, 2000 x 2048: 30 and 23 us).
 double launch_us(int tile, int kinds, const int64_t* items, const int64_t* steps) {
   int64_t count = 0;
   for (int i = 0; i < kinds; ++i) count += items[i];
@@ -99,9 +99,10 @@ Gemm grid_of(int tile, int64_t M, int64_t N) {
   g.tn = int(up(N, tile) / tile);
   return g;
 }
-// The tile of a product that runs alone; its K ranges if it may have them (the logits: on 128 x 128 tiles, in one round and of an even
-// number of steps, at least 16, each; their sum and the epilogue, launches of their own, taken as 14 us and the sum's traffic. 553 tokens, 722 ids, 1088 wide, fp32:
-// 35 us, 43 in one range; 300 tokens, 400 ids, 4000 wide: 28 and 117 us).
+// The tile of a product that runs alone; its K ranges if it may have them (the logits: on 128 x 128 tiles, in one round and
+// of an even number of steps, at least 16, each; their sum and the epilogue, launches of their own, taken as 14 us and the
+// sum's traffic. 553 tokens, 722 ids, 1088 wide, fp32: 35 us, 43 in one range; 300 tokens, 400 ids, 4000 wide: 28 and 117
+// us).
 Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
   Gemm best;
   double us = 0.0;
@@ -123,8 +124,8 @@ Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
   }
   return best;
 }
-// The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K; 0: not asked for) in one launch, and the K ranges of dx: each range
-// at least 16 steps long, the join of the ranges taken as its traffic and a launch.
+// The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K; 0: not asked for) in one launch, and the K ranges of dx:
+// each range at least 16 steps long, the join of the ranges taken as its traffic and a launch.
 void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wsteps, Gemm& dx, Gemm& dw) {
   double best = 0.0;
   dx.tile = 0;
@@ -521,8 +522,8 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (!last) mw.part = f32p(p.acc);
     }
     LossGemm2 both{};
-    // dw of a few tokens on a kernel of its own (48 tokens, 128256 x 4096: 247 us, 295 on the tiles' kernel), unless its tiles go into
-    // dx's launch in one round (64 tokens, 1000 x 64, dx and dw: 13 us in one launch, 20 in two)
+    // dw of a few tokens on a kernel of its own (48 tokens, 128256 x 4096: 247 us, 295 on the tiles' kernel), unless its
+    // tiles go into dx's launch in one round (64 tokens, 1000 x 64, dx and dw: 13 us in one launch, 20 in two)
     const bool short_dw = !p.f32 && first && last && rows <= kStreamTokens && (p.stream || !a->dx || p.dw.items() > 256);
     // otherwise one launch where both use the same tile, the longer tiles first
     const bool together = a->dx && a->dw && !p.stream && !short_dw && p.dx.tile == p.dw.tile;
