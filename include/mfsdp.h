@@ -420,7 +420,7 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  *   token_loss   optional, n fp32: l_r (neither weighted nor scaled; 0 for a token that does not count)
  *   lse          optional, n fp32: log sum_v exp z_rv of the (tempered) logits; 0 for a token that does not count
  *   dx, dw       optional, n x h and v x h of dtype: gradients of loss, overwritten (at least one of the five
- *                outputs has to be given)
+ *                outputs has to be given, unless n is 0)
  *   chunk_rows   0, or the most rows of x per pass where gradients are asked for (rounded up to 256): fewer rows take
  *                less workspace and more time. 0: as many as fit 2 GiB of 16-bit logits.
  * No output may overlap an input or another output.

@@ -160,7 +160,7 @@ int check(const mfsdp_head_loss* a, int64_t k, bool pointers) {
   if (a->chunk_rows < 0) return fail(MFSDP_E_INVALID, "chunk_rows must be >= 0");
   if (!pointers) return MFSDP_OK;
   if (!a->w || (a->n > 0 && !a->x)) return fail(MFSDP_E_INVALID, "x or w is NULL");
-  if (!a->loss && !a->token_loss && !a->lse && !a->dx && !a->dw)
+  if (a->n > 0 && !a->loss && !a->token_loss && !a->lse && !a->dx && !a->dw)
     return fail(MFSDP_E_INVALID, "every output is NULL");
   for (const void* p : {a->x, a->w, (const void*)a->token_weight, (const void*)a->loss, (const void*)a->token_loss,
                         (const void*)a->lse, (const void*)a->dx, (const void*)a->dw})

@@ -158,3 +158,22 @@ def test_a_training_step_with_both_losses_and_the_owner_optimizer():
     want, _, _ = oracle.adamw_step(bias, g, np.zeros(h), np.zeros(h), lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
                                    weight_decay=0.01, step=1)
     assert np.abs(from_dev(b.detach()) - want).max() <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", [synth.BF16, synth.F32])
+def test_no_token_at_all(dtype):
+    """An empty batch: loss 0, the head's gradient 0, the hidden states' gradient empty; on a stream of its own."""
+    import torch
+    from paper_2607_05895_amd import losses
+    rng = np.random.default_rng(4)
+    W = _leaf(_store(rng.standard_normal((300, 48)), dtype)[0], dtype)
+    X = torch.empty((2, 0, 48), dtype=W.dtype, device="cuda", requires_grad=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        loss = losses.linear_cross_entropy(X, W, torch.empty((2, 0), dtype=torch.int64, device="cuda"))
+        loss.backward()
+        nll = losses.token_losses(X, W, torch.empty((2, 0), dtype=torch.int64, device="cuda"))
+    torch.cuda.synchronize()
+    assert float(loss.detach()) == 0.0 and nll.shape == (2, 0)
+    assert X.grad.shape == X.shape and not W.grad.any()
