@@ -16,18 +16,24 @@ from torch.autograd.function import once_differentiable
 from . import native
 
 
+def _dense(t: torch.Tensor) -> torch.Tensor:
+    """t contiguous and 16-byte aligned, as the library takes it (labels shifted by one, ids[1:], are not)."""
+    t = t.detach().contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 def _rows(t: torch.Tensor, tail: int, what: str) -> torch.Tensor:
     """t with its leading dimensions as one; `tail` dimensions stay."""
     if t.dim() <= tail:
         raise ValueError(f"{what}: at least {tail + 1} dimensions are required, got shape {tuple(t.shape)}")
-    return t.detach().reshape(-1, *t.shape[t.dim() - tail:]).contiguous()
+    return _dense(t.reshape(-1, *t.shape[t.dim() - tail:]))
 
 
 class _HeadLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, grads, call):
         with torch.cuda.device(hidden.device):
-            x, w = _rows(hidden, 1, "hidden"), weight.detach().contiguous()
+            x, w = _rows(hidden, 1, "hidden"), _dense(weight)
             loss = torch.empty((), dtype=torch.float32, device=hidden.device)
             dx = torch.empty_like(x) if grads and ctx.needs_input_grad[0] else None
             dw = torch.empty_like(w) if grads and ctx.needs_input_grad[1] else None
@@ -66,8 +72,8 @@ def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: to
     _check_head(hidden, weight)
     if targets.shape != hidden.shape[:-1]:
         raise ValueError(f"targets: shape {tuple(targets.shape)} where {tuple(hidden.shape[:-1])} is required")
-    t = targets.reshape(-1).contiguous()
-    a = None if token_weight is None else token_weight.detach().reshape(-1).contiguous()
+    t = _dense(targets.reshape(-1))
+    a = None if token_weight is None else _dense(token_weight.reshape(-1))
 
     def call(x, w, **out):
         native.linear_xent_t(x, w, t, ignore_index=ignore_index, reduction=reduction, scale=scale, token_weight=a,
@@ -88,7 +94,7 @@ def linear_distillation(hidden: torch.Tensor, weight: torch.Tensor, top_ids: tor
         if t.shape != want:
             raise ValueError(f"{what}: shape {tuple(t.shape)} where {want} is required")
     ids, logits = _rows(top_ids, 1, "top_ids"), _rows(top_logits, 1, "top_logits")
-    a = None if token_weight is None else token_weight.detach().reshape(-1).contiguous()
+    a = None if token_weight is None else _dense(token_weight.reshape(-1))
 
     def call(x, w, **out):
         native.linear_distill_t(x, w, ids, logits, temperature=temperature, reduction=reduction, scale=scale,
@@ -106,6 +112,6 @@ def token_losses(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tens
         raise ValueError(f"targets: shape {tuple(targets.shape)} where {tuple(hidden.shape[:-1])} is required")
     with torch.cuda.device(hidden.device):
         out = torch.empty(targets.shape, dtype=torch.float32, device=hidden.device)
-        native.linear_xent_t(_rows(hidden, 1, "hidden"), weight.detach().contiguous(), targets.reshape(-1).contiguous(),
+        native.linear_xent_t(_rows(hidden, 1, "hidden"), _dense(weight), _dense(targets.reshape(-1)),
                              token_loss=out.view(-1), ignore_index=ignore_index)
     return out

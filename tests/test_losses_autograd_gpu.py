@@ -177,3 +177,27 @@ def test_no_token_at_all(dtype):
     torch.cuda.synchronize()
     assert float(loss.detach()) == 0.0 and nll.shape == (2, 0)
     assert X.grad.shape == X.shape and not W.grad.any()
+
+
+@pytest.mark.parametrize("dtype", [synth.BF16, synth.F32])
+def test_shifted_views(dtype):
+    """Next-token labels: ids[1:] beside hidden[:-1], and views that begin in the middle of 16 bytes, give what copies give."""
+    import torch
+    from paper_2607_05895_amd import losses
+    rng = np.random.default_rng(5)
+    T, v, h = 38, 500, 18
+    hid, w = (_leaf(_store(rng.standard_normal(s), dtype)[0], dtype) for s in ((T, h), (v + 1, h)))
+    ids = torch.from_numpy(rng.integers(0, v, T)).cuda()
+    a = torch.rand(T, device="cuda")
+    top, lg = torch.randint(0, v, (T, 3), device="cuda"), torch.randn(T, 3, device="cuda")
+
+    def grads(loss):
+        return [loss.detach(), *torch.autograd.grad(loss, (hid, w))]
+
+    got = grads(losses.linear_cross_entropy(hid[1:], w[1:], ids[1:], token_weight=a[1:]))
+    want = grads(losses.linear_cross_entropy(hid[1:].clone(), w[1:].clone(), ids[1:].clone(), token_weight=a[1:].clone()))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    got = grads(losses.linear_distillation(hid[1:], w[1:], top[1:], lg[1:]))
+    want = grads(losses.linear_distillation(hid[1:].clone(), w[1:].clone(), top[1:].clone(), lg[1:].clone()))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert torch.equal(losses.token_losses(hid[:-1], w, ids[1:]), losses.token_losses(hid[:-1].clone(), w, ids[1:].clone()))
