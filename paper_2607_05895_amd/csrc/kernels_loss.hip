@@ -1588,8 +1588,9 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
 // dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). A workgroup of four waves keeps CT
 // columns of x in registers and goes through blocks of 64 rows (ids), gridDim.y blocks apart: both parts of the next block of
 // dz are on their way while this one's product goes out, through LDS, so that a wave stores whole rows of CT columns. (48
-// tokens, 128256 x 4096, 1.05 GB: 245 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel
-// more.)
+// tokens, 128256 x 4096, 1.05 GB: 234 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel
+// more.) Non-temporal stores: with plain ones it takes 245 us, and what reads w after it 284 us instead of 233, waiting for
+// the caches to write dw back (the whole call 728 -> 670 us).
 template <int KS>
 __global__ __launch_bounds__(256) void loss_dw_kernel(const LossGemm a) {
   constexpr int NPAN = 2 * KS, NJ = KS <= 2 ? 2 : 1, CT = 128 * NJ, CB = CT / 32;  // panels of 16 tokens; columns, in blocks of 32
@@ -1689,7 +1690,7 @@ __global__ __launch_bounds__(256) void loss_dw_kernel(const LossGemm a) {
         if (row < a.rows) {
           uint16_t* dst = (uint16_t*)a.out + int64_t(row) * a.ldo + c;
           if (c + 8 <= a.cols) {
-            *(gptr<u32x4_a2>)dst = val;
+            __builtin_nontemporal_store(u32x4_a2(val), (gptr<u32x4_a2>)dst);
           } else {
 #pragma unroll
             for (int t = 0; t < 8; ++t)
