@@ -1426,6 +1426,12 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
     nk = min(a.kper, a.nk - k0);
     return it - s * a.tiles;
   };
+  // This wave's LDS reads have returned. The loads behind the next barrier overwrite what they read; without this the
+  // compiler may let a product, and the wait for its operands, slide past that barrier.
+  auto reads_done = [] {
+    LOSS_WAIT_LGKM0();
+    __builtin_amdgcn_sched_barrier(0);
+  };
   int k0, nk, tile = range(item, k0, nk);
 #pragma unroll
   for (int s = 0; s < NST - 1; ++s) issue(tile, k0 + min(s, nk - 1), s);
@@ -1438,7 +1444,8 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
     int cs = 0;
     for (int kt = 0; kt < nk; ++kt) {
       LOSS_WAIT_VMCNT((NST - 2) * LOADS);  // this wave's loads of step kt
-      __builtin_amdgcn_s_barrier();        // everybody's; and step kt - 1 is read
+      reads_done();                        // (of step kt - 1, or of the K halves' sums)
+      __builtin_amdgcn_s_barrier();        // everybody's
       issue(tile, k0 + min(kt + NST - 1, nk - 1), cs == 0 ? NST - 1 : cs - 1);
       const uint8_t* sb = smem + cs * STAGE;
 #pragma unroll
@@ -1468,6 +1475,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
       cs = cs + 1 == NST ? 0 : cs + 1;
     }
     LOSS_WAIT_VMCNT(0);
+    reads_done();
     __builtin_amdgcn_s_barrier();
     const int done = tile, split = item / a.tiles;
     item += gridDim.x;

@@ -646,3 +646,34 @@ def test_helpers_refuse_what_does_not_fit():
     small = torch.empty(256, dtype=torch.uint8, device="cuda")
     with pytest.raises(native.MfsdpError, match="too small"):
         native.linear_xent_t(x, w, t, loss=loss, workspace=small)
+
+
+@pytest.mark.parametrize("n,v,h", [(20, 40003, 1032), (50, 50257, 768), (128, 33001, 1544)])
+def test_few_tokens_many_steps(n, v, h):
+    """The products for a few tokens with more tiles than workgroups and rings that go round many times: the oracle's results, and
+    the same bits from each of twenty calls, on a busy chip too."""
+    import torch
+    rng = np.random.default_rng(41)
+    x, w, x64, w64 = _inputs(rng, n, v, h, BF16)
+    t = _labels(rng, n, v)
+    _say(n, v, h)
+    got = _call("xent", x, w, BF16, t)
+    ref = _Ref(OL.linear_xent(x64, w64, t), t >= 0, None, "mean", 1.0)
+    q = np.zeros((n, v), bool)
+    q[np.nonzero(t >= 0)[0], t[t >= 0]] = True
+    _check(got, ref, x64, w64, BF16, q, what=f"few tokens {n}x{v}x{h}")
+    _check_loss(got, ref)
+    xd, wd, td = to_dev(x, BF16), to_dev(w, BF16), torch.from_numpy(t).cuda()
+    args = native.head_loss_args_t(xd, wd, dx=xd, dw=wd)
+    wss, streams = [native.head_loss_workspace_t(args) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty(n, device="cuda"), torch.empty_like(xd), torch.empty_like(wd)] for _ in range(2)]
+    first = None
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, ws, o in zip(streams, wss, outs):
+            with torch.cuda.stream(s):
+                native.linear_xent_t(xd, wd, td, token_loss=o[0], dx=o[1], dw=o[2], workspace=ws)
+        torch.cuda.synchronize()
+        bits = [_bits(o) for o in outs]
+        first = first or bits[0]
+        assert all(torch.equal(a, b) for o in bits for a, b in zip(o, first)), i
