@@ -471,7 +471,8 @@ int mfsdp_linear_xent(const mfsdp_head_loss* args, const void* targets, int32_t 
  *   ids          n x k vocabulary ids, int32 (id_bytes 4) or int64 (8), in any order; a negative one marks an empty slot,
  *                one >= v makes l_r NaN; an id that fills several slots takes the sum of their q. A token without a
  *                filled slot does not count.
- *   logits       n x k teacher logits of logit_dtype (-inf: q = 0); those of empty slots are not looked at
+ *   logits       n x k teacher logits of logit_dtype (-inf: q = 0; +inf or NaN makes l_r NaN); those of empty slots are not
+ *                looked at
  *   k            1 .. MFSDP_MAX_TOP_LOGITS;  temperature > 0 (l_r is not multiplied by temperature^2: use scale)
  * Everything else as mfsdp_linear_xent. */
 int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t id_bytes, const void* logits,

@@ -861,7 +861,7 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
         id[i] = v >= 0 && v < l.v ? int(v) : -1;
         lg[i] = !l.logits ? 0.0f : label_logit(l, at) * l.inv_t;
         m = fmaxf(m, lg[i]);
-        if (!(lg[i] == lg[i])) bad = true;  // a NaN teacher logit
+        if (!(lg[i] < __builtin_inff())) bad = true;  // a teacher logit of +inf or NaN has no softmax
       }
     }
   }
@@ -1159,7 +1159,7 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
         const float ls = log1pf(s), lse = m + ls;
         float loss = 0.0f;
         if (on != 0.0f) {
-          loss = (ent + d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for an id outside the vocabulary)
+          loss = (ent + d + ls + a.z_loss * lse * lse) * on;  // (on is NaN for a label that has no loss)
         }
         const float4 rw = {m, s, on != 0.0f ? wt * on : 0.0f, 2.0f * a.z_loss * lse};
         a.row[r] = rw;

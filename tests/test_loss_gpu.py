@@ -677,3 +677,27 @@ def test_few_tokens_many_steps(n, v, h):
         bits = [_bits(o) for o in outs]
         first = first or bits[0]
         assert all(torch.equal(a, b) for o in bits for a, b in zip(o, first)), i
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("n,v", [(5, 70), (300, 400), (20, 4500)])
+def test_a_teacher_logit_of_infinity_or_nan_gives_nan(n, v, value, dtype):
+    """With gradients and without: its token's loss, dx and the reduced loss are NaN, the other tokens stay."""
+    rng = np.random.default_rng(42)
+    x, w, _, _ = _inputs(rng, n, v, 24, dtype)
+    ids, lg = _teacher(rng, n, v, 5, empty=0.0)
+    bad = lg.copy()
+    bad[3, 2] = value
+    _say(n, v, value, dtype)
+    others = np.arange(n) != 3
+    for lgt in (F32, BF16):
+        store = (lambda a: synth.f32_to_bf16_bits(a)) if lgt == BF16 else (lambda a: a)
+        clean = _call("distill", x, w, dtype, (ids, store(lg), lgt), reduction="sum")
+        for outs in (("loss", "token_loss", "lse", "dx", "dw"), ("loss", "token_loss")):
+            got = _call("distill", x, w, dtype, (ids, store(bad), lgt), outs=outs, reduction="sum")
+            assert np.isnan(got["token_loss"][3]) and np.isnan(got["loss"][0]), outs
+            np.testing.assert_array_equal(got["token_loss"][others], clean["token_loss"][others])
+        got = _call("distill", x, w, dtype, (ids, store(bad), lgt), reduction="sum")
+        assert np.isnan(got["dx"][3]).all() and np.isnan(got["dw"]).all()
+        np.testing.assert_array_equal(got["dx"][others], clean["dx"][others])
