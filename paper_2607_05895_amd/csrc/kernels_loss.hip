@@ -859,7 +859,7 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
       if (!none) {
         bad |= v < 0 || v >= l.v;
         id[i] = v >= 0 && v < l.v ? int(v) : -1;
-        lg[i] = !l.logits ? 0.0f : label_logit(l, at) * l.inv_t;
+        lg[i] = !l.logits ? 0.0f : label_logit(l, at);
         m = fmaxf(m, lg[i]);
         if (!(lg[i] < __builtin_inff())) bad = true;  // a teacher logit of +inf or NaN has no softmax
       }
@@ -869,10 +869,12 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
   bad = __any(bad);
   // (a row whose slots are all empty, or all of logit -inf, teaches nothing)
   const bool on = m > -__builtin_inff();
+  // (differences first: a large logit over a small temperature may be beyond fp32)
   float e[PER], s = 0.0f;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    e[i] = on && lg[i] > -__builtin_inff() ? expf(lg[i] - m) : 0.0f;
+    lg[i] = (lg[i] - m) * l.inv_t;
+    e[i] = on && lg[i] > -__builtin_inff() ? expf(lg[i]) : 0.0f;
     s += e[i];
   }
   s = wave_sum(s);
@@ -880,7 +882,7 @@ __device__ __forceinline__ void prep_labels(const LossPrep& a, int64_t r) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     sum[i] = q[i] = on ? e[i] / s : 0.0f;
-    if (q[i] > 0.0f) ent += q[i] * ((lg[i] - m) - logf(s));
+    if (q[i] > 0.0f) ent += q[i] * (lg[i] - logf(s));
   }
   // an id given more than once: its first slot takes the weights of all, the others become empty
   if (l.k > 1) {

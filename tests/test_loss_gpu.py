@@ -701,3 +701,20 @@ def test_a_teacher_logit_of_infinity_or_nan_gives_nan(n, v, value, dtype):
         got = _call("distill", x, w, dtype, (ids, store(bad), lgt), reduction="sum")
         assert np.isnan(got["dx"][3]).all() and np.isnan(got["dw"]).all()
         np.testing.assert_array_equal(got["dx"][others], clean["dx"][others])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_teacher_logits_over_a_small_temperature(dtype):
+    """Finite teacher logits whose quotient by the temperature is beyond fp32: their softmax is still one."""
+    rng = np.random.default_rng(43)
+    n, v, h, temp = 9, 90, 24, 2.0 ** -10
+    x, w, x64, w64 = _inputs(rng, n, v, h, dtype, x_scale=2.0 ** -10)
+    ids = np.stack([rng.permutation(v)[:4] for _ in range(n)])
+    lg = np.array([3e38, 2e38, -3e38, 3e38], np.float32) * np.ones((n, 1), np.float32)
+    lg[1] = [1e37, 1e37, 1e37, -3e38]
+    got = _call("distill", x, w, dtype, (ids, lg, F32), temperature=temp)
+    ref = _Ref(OL.linear_distill(x64, w64, ids, lg.astype(np.float64), temperature=temp), np.ones(n, bool), None, "mean", 1.0)
+    q = np.zeros((n, v), bool)
+    q[np.arange(n)[:, None], ids] = True
+    _check(got, ref, x64, w64, dtype, q, inv_t=1 / temp, what=f"small temperature {dtype}")
+    _check_loss(got, ref)
