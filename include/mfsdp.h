@@ -414,7 +414,7 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
 /* n tokens with hidden states x through an output head w: logits z = x w^T (n x v), which are never held as a whole (a
  * chunk of rows at 16 bits each where gradients are asked for, none otherwise).
  *   x, w         n x h and v x h of dtype (F32 or BF16), read only; 0 <= n <= 2^25, 1 <= v, h <= 2^20
- *   reduction, scale  an mfsdp_reduction and a finite factor; the gradients are those of loss
+ *   reduction, scale  an mfsdp_reduction and a factor that is finite in fp32; the gradients are those of loss
  *   token_weight optional n fp32 weights a_r (NULL: 1)
  *   loss         optional, 1 fp32: the reduced loss
  *   token_loss   optional, n fp32: l_r (neither weighted nor scaled; 0 for a token that does not count)
@@ -458,7 +458,7 @@ size_t mfsdp_head_loss_workspace_size(const mfsdp_head_loss* args, int32_t k);
 /* Softmax cross entropy with hard labels: l_r = lse_r - z_{r, t_r} + z_loss lse_r^2.
  *   targets      n labels t_r, int32 (target_bytes 4) or int64 (8). A token with t_r = ignore_index does not count;
  *                any other label outside [0, v) makes its l_r, and with it loss and gradients, NaN.
- *   z_loss       >= 0
+ *   z_loss       >= 0, finite in fp32
  * Enqueued on `stream`, with no host synchronisation and no allocation. The workspace (device, 256-byte aligned, >= the
  * size query) must not be in use by another call still running. Returns MFSDP_OK, MFSDP_E_INVALID, MFSDP_E_WORKSPACE or
  * MFSDP_E_HIP; on an argument error nothing is enqueued. n = 0 gives loss 0 and dw 0. */
@@ -473,7 +473,8 @@ int mfsdp_linear_xent(const mfsdp_head_loss* args, const void* targets, int32_t 
  *                filled slot does not count.
  *   logits       n x k teacher logits of logit_dtype (-inf: q = 0; +inf or NaN makes l_r NaN); those of empty slots are not
  *                looked at
- *   k            1 .. MFSDP_MAX_TOP_LOGITS;  temperature > 0 (l_r is not multiplied by temperature^2: use scale)
+ *   k            1 .. MFSDP_MAX_TOP_LOGITS;  temperature > 0, its inverse a normal and scale / temperature a finite number in
+ *                fp32 (l_r is not multiplied by temperature^2: use scale)
  * Everything else as mfsdp_linear_xent. */
 int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t id_bytes, const void* logits,
                          int32_t logit_dtype, int32_t k, double temperature, void* workspace, size_t workspace_bytes,

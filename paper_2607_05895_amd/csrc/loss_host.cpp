@@ -156,7 +156,7 @@ int check(const mfsdp_head_loss* a, int64_t k, bool pointers) {
   if (k < 1 || k > kLossMaxTop) return fail(MFSDP_E_INVALID, "k must be in [1, MFSDP_MAX_TOP_LOGITS]");
   if (a->dtype != MFSDP_F32 && a->dtype != MFSDP_BF16) return fail(MFSDP_E_INVALID, "unsupported dtype");
   if (a->reduction != MFSDP_SUM && a->reduction != MFSDP_MEAN) return fail(MFSDP_E_INVALID, "unknown reduction");
-  if (!std::isfinite(a->scale)) return fail(MFSDP_E_INVALID, "scale must be finite");
+  if (!std::isfinite(float(a->scale))) return fail(MFSDP_E_INVALID, "scale must be finite in fp32");
   if (a->chunk_rows < 0) return fail(MFSDP_E_INVALID, "chunk_rows must be >= 0");
   if (!pointers) return MFSDP_OK;
   if (!a->w || (a->n > 0 && !a->x)) return fail(MFSDP_E_INVALID, "x or w is NULL");
@@ -596,7 +596,7 @@ int mfsdp_linear_xent(const mfsdp_head_loss* args, const void* targets, int32_t 
   if (!targets && args->n > 0) return fail(MFSDP_E_INVALID, "targets is NULL");
   if (target_bytes != 4 && target_bytes != 8) return fail(MFSDP_E_INVALID, "target_bytes must be 4 or 8");
   if (!aligned16(targets)) return fail(MFSDP_E_INVALID, "pointers must be 16-byte aligned");
-  if (!std::isfinite(z_loss) || z_loss < 0.0) return fail(MFSDP_E_INVALID, "z_loss must be >= 0");
+  if (!std::isfinite(float(z_loss)) || z_loss < 0.0) return fail(MFSDP_E_INVALID, "z_loss must be >= 0 and finite in fp32");
   return run(args, 1, Labels{targets, nullptr, target_bytes, 0, ignore_index, 1.0, z_loss}, workspace, workspace_bytes, stream);
 }
 
@@ -608,7 +608,9 @@ int mfsdp_linear_distill(const mfsdp_head_loss* args, const void* ids, int32_t i
   if (id_bytes != 4 && id_bytes != 8) return fail(MFSDP_E_INVALID, "id_bytes must be 4 or 8");
   if (logit_dtype != MFSDP_F32 && logit_dtype != MFSDP_BF16) return fail(MFSDP_E_INVALID, "unsupported logit dtype");
   if (!aligned16(ids) || !aligned16(logits)) return fail(MFSDP_E_INVALID, "pointers must be 16-byte aligned");
-  if (!std::isfinite(temperature) || !(temperature > 0.0)) return fail(MFSDP_E_INVALID, "temperature must be > 0");
+  // (the kernels multiply by its inverse)
+  if (!(temperature > 0.0) || !std::isnormal(float(1.0 / temperature)) || !std::isfinite(float(args->scale / temperature)))
+    return fail(MFSDP_E_INVALID, "temperature must be > 0, 1 / temperature normal and scale / temperature finite in fp32");
   return run(args, k, Labels{ids, logits, id_bytes, logit_dtype, 0, temperature, 0.0}, workspace, workspace_bytes, stream);
 }
 

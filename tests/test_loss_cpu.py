@@ -128,3 +128,35 @@ def test_bad_scale_arguments_are_refused(grad, numel, dt, factor):
 def test_struct_matches_the_header():
     """8-byte fields and pairs of 4-byte ones: no padding anywhere."""
     assert ctypes.sizeof(native.HeadLoss) == 8 * 14
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e39, 1e300])
+def test_a_scale_beyond_fp32_is_refused(scale):
+    a = _args(scale=scale)
+    for call in (lambda: native.mfsdp_linear_xent(a, FAKE, 8, -100, 0.0, FAKE * 16, 1 << 50),
+                 lambda: native.mfsdp_linear_distill(a, FAKE, 8, FAKE, native.F32, 4, 1.0, FAKE * 16, 1 << 50),
+                 lambda: native.mfsdp_head_loss_workspace_size(a)):
+        with pytest.raises(native.MfsdpError, match="fp32") as ei:
+            call()
+        assert ei.value.status == native.E_INVALID
+
+
+@pytest.mark.parametrize("scale,temperature", [(1.0, 1e-39), (1.0, 1e-300), (1.0, 1e39), (1.0, 1e300), (1e30, 1e-9), (-1e30, 1e-9)])
+def test_a_temperature_beyond_fp32_is_refused(scale, temperature):
+    """1 / temperature infinite or denormal, scale / temperature infinite: the results would be NaN or 0. (A workspace that
+    is too small: a call that is not refused for its temperature is refused for that.)"""
+    with pytest.raises(native.MfsdpError, match="temperature") as ei:
+        native.mfsdp_linear_distill(_args(scale=scale), FAKE, 8, FAKE, native.F32, 4, temperature, FAKE * 16, 1 << 10)
+    assert ei.value.status == native.E_INVALID
+
+
+@pytest.mark.parametrize("temperature", [1e-37, 1e-3, 1e3, 1e37])
+def test_far_temperatures_are_taken(temperature):
+    with pytest.raises(native.MfsdpError, match="too small"):
+        native.mfsdp_linear_distill(_args(), FAKE, 8, FAKE, native.F32, 4, temperature, FAKE * 16, 1 << 10)
+
+
+def test_a_z_loss_beyond_fp32_is_refused():
+    with pytest.raises(native.MfsdpError, match="z_loss") as ei:
+        native.mfsdp_linear_xent(_args(), FAKE, 8, -100, 1e39, FAKE * 16, 1 << 10)
+    assert ei.value.status == native.E_INVALID
