@@ -160,3 +160,15 @@ def test_a_z_loss_beyond_fp32_is_refused():
     with pytest.raises(native.MfsdpError, match="z_loss") as ei:
         native.mfsdp_linear_xent(_args(), FAKE, 8, -100, 1e39, FAKE * 16, 1 << 10)
     assert ei.value.status == native.E_INVALID
+
+
+def test_one_token_more_than_a_call_takes_is_refused():
+    size = lambda n: native.mfsdp_head_loss_workspace_size(_args(n=n))  # noqa: E731
+    assert size(1 << 25) > 0
+    for n in ((1 << 25) + 1, 1 << 26):
+        with pytest.raises(native.MfsdpError) as ei:
+            size(n)
+        assert ei.value.status == native.E_INVALID
+        with pytest.raises(native.MfsdpError) as ei:
+            native.mfsdp_linear_xent(_args(n=n), FAKE, 8, -100, 0.0, FAKE * 16, 1 << 50)
+        assert ei.value.status == native.E_INVALID
