@@ -421,8 +421,9 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  *   lse          optional, n fp32: log sum_v exp z_rv of the (tempered) logits; 0 for a token that does not count
  *   dx, dw       optional, n x h and v x h of dtype: gradients of loss, overwritten (at least one of the five
  *                outputs has to be given, unless n is 0)
- *   chunk_rows   0, or the most rows of x per pass where gradients are asked for (rounded up to 256): fewer rows take
- *                less workspace and more time. 0: as many as fit 2 GiB of 16-bit logits.
+ *   chunk_rows   0, or the most rows of x per pass (rounded up to 256). A row of a pass takes 2 v bytes (F32: 8 v) where
+ *                gradients are asked for; more than one pass takes more time, and with dw another 4 v h bytes for its sum.
+ *                0: with gradients as many rows as fit 2 GiB of 16-bit logits; without, as many as take the same workspace.
  * No output may overlap an input or another output.
  * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0. The other rows
  * and w have to be finite: an infinity or a NaN there may make any result NaN. A BF16 logit that overflows to -inf is a
@@ -451,8 +452,9 @@ typedef struct {
 } mfsdp_head_loss;
 
 /* Bytes of device workspace for mfsdp_linear_xent (k = 1) and mfsdp_linear_distill with these arguments: the chunk's rows of
- * x and (for gradients) its logits, a copy of w for F32 (two fp16 parts) and for h that are no multiple of 8, and for n beyond
- * one chunk an fp32 sum of dw. Of the pointers only whether dx and dw are NULL is looked at. 0 on invalid arguments. */
+ * x and (for gradients) its logits, a copy of w for F32 (two fp16 parts) and for h that are no multiple of 8, for dx a few
+ * hundred MiB of partial sums at most, and for n beyond one chunk an fp32 sum of dw. Of the pointers only whether dx and dw
+ * are NULL is looked at. Fewer tokens, fewer outputs or a smaller k never need more. 0 on invalid arguments. */
 size_t mfsdp_head_loss_workspace_size(const mfsdp_head_loss* args, int32_t k);
 
 /* Softmax cross entropy with hard labels: l_r = lse_r - z_{r, t_r} + z_loss lse_r^2.

@@ -71,6 +71,10 @@ struct Plan {
 // The most tokens, and the fewest ids, of the products for a few tokens.
 constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
 
+constexpr int64_t kMinRange = 16, kMaxRanges = 64;        // K steps of a range at least; ranges of dx at most
+constexpr int64_t kMaxItems = 512;                        // tiles of the logits in K ranges at most
+constexpr int64_t kRangeBytes = int64_t(256) << 20;       // room for dx's ranges (see range_room)
+
 // A launch's time in us on `tile` x `tile` tiles, items[i] of steps[i] K steps each: what the chip's workgroups share, or the
 // longest item if that is more, and half of the shortest kind for the uneven end. Measured: a step of 32 takes 0.74 us on a
 // 256 x 256 tile (1.45 PFLOP/s over 256 CUs) and a tile's start and epilogue 8 us; on 128 x 128 tiles 0.3 and 5 us with a CU
@@ -100,7 +104,7 @@ Gemm grid_of(int tile, int64_t M, int64_t N) {
   return g;
 }
 // The tile of a product that runs alone; its K ranges if it may have them (the logits: on 128 x 128 tiles, in one round and
-// of an even number of steps, at least 16, each; their sum and the epilogue, launches of their own, taken as 14 us and the
+// of an even number of steps, at least kMinRange, each; their sum and the epilogue, launches of their own, taken as 14 us and the
 // sum's traffic. 553 tokens, 722 ids, 1088 wide, fp32: 35 us, 43 in one range; 300 tokens, 400 ids, 4000 wide: 28 and 117
 // us).
 Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
@@ -108,7 +112,7 @@ Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
   double us = 0.0;
   for (int tile : {kLossTile, kLossTileSmall}) {
     Gemm g = grid_of(tile, M, N);
-    const int64_t tiles = g.items(), most = ranges && tile == kLossTileSmall ? std::min<int64_t>(512 / tiles, steps / 16) : 1;
+    const int64_t tiles = g.items(), most = ranges && tile == kLossTileSmall ? std::min<int64_t>(kMaxItems / tiles, steps / kMinRange) : 1;
     for (int64_t s = 1; s == 1 || s <= most; ++s) {
       const int64_t kper = s == 1 ? steps : up((steps + s - 1) / s, 2), items = tiles * s;
       if (s > 1 && (steps + kper - 1) / kper != s) continue;
@@ -125,15 +129,16 @@ Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
   return best;
 }
 // The tile of dx (n x h, xsteps of K) and dw (v x h, wsteps of K; 0: not asked for) in one launch, and the K ranges of dx:
-// each range at least 16 steps long, the join of the ranges taken as its traffic and a launch.
-void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wsteps, Gemm& dx, Gemm& dw) {
+// at most kMaxRanges of at least kMinRange steps, whose results fit `room` bytes; their join is taken as its traffic and a
+// launch.
+void choose_grads(int64_t n, int64_t v, int64_t h, int64_t xsteps, int64_t wsteps, int64_t room, Gemm& dx, Gemm& dw) {
   double best = 0.0;
   dx.tile = 0;
   for (int tile : {kLossTile, kLossTileSmall}) {
     const Gemm x = grid_of(tile, n, h), w = grid_of(tile, v, h);
-    for (int s = 1; s <= 64 && (s == 1 || xsteps / s >= 16); ++s) {
+    for (int s = 1; s <= kMaxRanges && (s == 1 || xsteps / s >= kMinRange); ++s) {
       const int64_t kper = (xsteps + s - 1) / s;
-      if ((xsteps + kper - 1) / kper != s) continue;
+      if ((xsteps + kper - 1) / kper != s || (s > 1 && x.items() * s * tile * tile * 4 > room)) continue;
       const int64_t items[2] = {x.items() * s, wsteps ? w.items() : 0}, steps[2] = {kper, wsteps};
       double us = launch_us(tile, 2, items, steps);
       if (s > 1) us += 6.0 + double(items[0]) * tile * tile * 8.0 / 4.9e6;
@@ -168,6 +173,28 @@ int check(const mfsdp_head_loss* a, int64_t k, bool pointers) {
   return MFSDP_OK;
 }
 
+// Room for K ranges: a bound over what the choices above may take, not what this call takes. A call over fewer rows may want
+// more ranges than one over many, and a workspace that is enough for many rows has to be enough for fewer; so each bound
+// grows with the call's rows alone.
+//   dx: kRangeBytes or a quarter of a pass's rows (pass_bytes), whichever is more. Of 38000 calls drawn over all sizes 54
+//   would be more than 1 % faster with ranges beyond that by launch_us, and none more than 5 %.
+int64_t range_room(const Plan& p, int64_t pass_bytes) {
+  const int64_t steps = (p.f32 ? kLossMaxSeg : 2) * (up(p.v, 32) / 32), most = std::min(kMaxRanges, steps / kMinRange);
+  return most < 2 ? 0 : std::min(std::max(kRangeBytes, pass_bytes / 4), p.n_pad * p.hp * 4 * most);
+}
+int64_t logit_range_room(const Plan& p) {
+  constexpr int64_t T = kLossTileSmall;
+  const int64_t steps = p.nseg * p.hk / 32, tn = up(p.v, T) / T;
+  if (steps / kMinRange < 2 || tn > kMaxItems / 2) return 0;
+  return std::min(kMaxItems, p.n_pad / T * tn * (steps / kMinRange)) * T * T * 4;
+}
+// dx of a few tokens: a workgroup per CU, in ranges of at least eight steps.
+int64_t stream_ranges(const Plan& p, int stream) {
+  const int64_t kt = stream_step(stream), steps = up(p.v, kt) / kt, tiles = p.hp / 256;
+  return std::max<int64_t>(1, std::min(steps / 8, (256 + tiles - 1) / tiles));
+}
+
+// The workspace grows, or stays, with the rows, the outputs and k.
 Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   Plan p;
   p.f32 = a->dtype == MFSDP_F32;
@@ -185,57 +212,59 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   p.hp = up(p.h, 256);
   p.copy = p.f32 || p.h % 8 != 0;
   p.ldw = p.copy ? p.hk : p.h;
-  if (!p.copy && p.n > 0 && p.n <= kStreamTokens && p.v >= kStreamIds) {
+  const int64_t es = 2 * p.parts, vsteps = up(p.v, 32) / 32;
+  // bytes of a row of x in a pass over many tokens, with gradients and without
+  const int64_t loss_row = p.hp * es + p.vp / kLossGroup * 8 + k * 4 + 16;
+  const int64_t grad_row = loss_row + p.vp * 2 * (p.f32 ? 2 : 1) + (p.f32 ? p.vp * 4 + 5 : 0);
+  int64_t with_grads = 0;  // rows of a pass
+  const bool streams = !p.copy && p.v >= kStreamIds;  // where the tokens are few
+  if (streams && p.n > 0 && p.n <= kStreamTokens) {
     p.stream = p.n <= 32 ? 1 : p.n <= 64 ? 2 : 4;
     p.group = 32;
     p.chunk = p.n_pad = 32 * p.stream;
   } else {
     p.n_pad = up(std::max<int64_t>(p.n, 1), 256);
-    int64_t most = kMaxChunk;
-    if (p.grads) most = std::min(most, std::max<int64_t>(256, kLogitBytes / (2 * p.vp) / 256 * 256));
-    if (a->chunk_rows > 0) most = std::min(most, up(a->chunk_rows, 256));
-    p.chunk = std::min(p.n_pad, most);
+    const int64_t asked = a->chunk_rows > 0 ? std::min(kMaxChunk, up(a->chunk_rows, 256)) : kMaxChunk;
+    with_grads = std::min({p.n_pad, asked, std::max<int64_t>(256, kLogitBytes / (2 * p.vp) / 256 * 256)});
+    p.chunk = with_grads;
+    const int64_t slots = (kLossMaxTop - k) * 4;
+    if (!p.grads)  // as many rows as take the bytes of those with gradients, with the most slots a row (the same for any k)
+      p.chunk = std::min({p.n_pad, asked, std::max(with_grads, with_grads * (grad_row + slots) / (loss_row + slots) / 256 * 256)});
   }
-  const int64_t vsteps = up(p.v, 32) / 32, groups = (p.vp + p.group - 1) / p.group;
+  const int64_t groups = (p.vp + p.group - 1) / p.group;
   // many tokens: the logits' lanes (rows) store whole lines; few: a row's partials are read in one piece
   p.gstep = p.chunk > 256 ? p.chunk : 1;
   p.rstep = p.chunk > 256 ? 1 : groups;
-  size_t part = 0;
+  const int64_t rows = std::min(p.chunk, std::max<int64_t>(p.n, 1)), wsteps = p.out_nseg * up(rows, 32) / 32;
+  int64_t part = 0;
   if (p.stream) {
     if (a->dx) {
-      // a workgroup per CU, in ranges of at least eight steps
-      const int64_t kt = stream_step(p.stream), steps = up(p.v, kt) / kt, tiles = p.hp / 256;
-      const int64_t splits = std::max<int64_t>(1, std::min(steps / 8, (256 + tiles - 1) / tiles));
+      const int64_t kt = stream_step(p.stream), steps = up(p.v, kt) / kt, splits = stream_ranges(p, p.stream);
       p.dx.nk = int(steps);
-      p.dx.tn = int(tiles);
+      p.dx.tn = int(p.hp / 256);
       p.dx.kper = int((steps + splits - 1) / splits);
       p.dx.splits = int((steps + p.dx.kper - 1) / p.dx.kper);
-      part = size_t(p.dx.splits) * size_t(p.chunk * p.hp) * 4;
+      part = splits * p.chunk * p.hp * 4;
     }
   } else {
-    p.logits = choose(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.nseg * p.hk / 32, true);
+    p.logits = choose(rows, p.v, p.nseg * p.hk / 32, true);
     p.logits.nk = int(p.hk / 32);
-    if (p.logits.splits > 1) part = size_t(p.logits.items()) * size_t(p.logits.tile) * p.logits.tile * 4;
+    part = logit_range_room(p);
+    if (a->dx) {
+      const int64_t room = range_room(p, with_grads * grad_row);
+      choose_grads(rows, p.v, p.h, p.out_nseg * vsteps, a->dw ? wsteps : 0, room, p.dx, p.dw);
+      p.dx.nk = int(vsteps);
+      part = std::max(part, room);
+      if (streams) part = std::max(part, stream_ranges(p, 4) * kStreamTokens * p.hp * 4);  // a call over few tokens
+    }
   }
-  const int64_t wsteps = p.out_nseg * up(std::min(p.chunk, std::max<int64_t>(p.n, 1)), 32) / 32;
-  if (a->dx && !p.stream) {
-    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.out_nseg * vsteps, a->dw ? wsteps : 0, p.dx, p.dw);
-    p.dx.nk = int(vsteps);
-    // room for the ranges of dx alone too: a call with fewer outputs never needs more workspace
-    Gemm alone, none;
-    choose_grads(std::min(p.chunk, std::max<int64_t>(p.n, 1)), p.v, p.h, p.out_nseg * vsteps, 0, alone, none);
-    for (const Gemm& g : {p.dx, alone})
-      if (g.splits > 1) part = std::max(part, size_t(g.items()) * size_t(g.tile) * g.tile * 4);
-  } else if (a->dw) {
-    p.dw = choose(p.v, p.h, wsteps, false);
-  }
+  if (a->dw && (p.stream || !a->dx)) p.dw = choose(p.v, p.h, wsteps, false);
   size_t o = 0;
   auto take = [&](int64_t bytes) {
     const size_t at = o;
     o += size_t(up(bytes, 256));
     return at;
   };
-  const int64_t es = 2 * p.parts;
   p.id = take(p.n_pad * k * 4);
   p.q = take(p.n_pad * k * 4);
   p.ent = take(p.n_pad * 4);
@@ -251,16 +280,19 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
     p.inv = take(2 * 4);
     p.xmax = take(p.n_pad * 4);
     p.wmax = take(kLossMaxima * 4);
-    p.row_most = take(p.chunk * 4);
-    p.most = take(std::max<int64_t>(256, p.chunk / 32) * 4);
   }
   p.xb = take(p.chunk * p.hp * es);
   if (p.copy) p.wb = take(p.v * p.ldw * es);
   if (p.grads) {
-    p.codes = take(p.chunk * p.vp * 2 * p.dz_parts);
-    if (p.f32) p.z32 = take(p.chunk * p.vp * 4);
+    // (up to 128 tokens on the tiles' kernels: two parts of 256 rows, which 129 tokens keep room for)
+    p.codes = take(std::max(p.chunk * p.dz_parts, streams || p.f32 ? 0 : int64_t(512)) * p.vp * 2);
+    if (p.f32) {
+      p.z32 = take(p.chunk * p.vp * 4);
+      p.row_most = take(p.chunk * 4);
+      p.most = take(std::max<int64_t>(256, p.chunk / 32) * 4);
+    }
   }
-  p.part = take(int64_t(part));
+  p.part = take(part);
   if (a->dw && p.chunk < p.n) p.acc = take(p.vp * p.hp * 4);
   p.bytes = o;
   return p;

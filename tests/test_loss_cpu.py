@@ -172,3 +172,46 @@ def test_one_token_more_than_a_call_takes_is_refused():
         with pytest.raises(native.MfsdpError) as ei:
             native.mfsdp_linear_xent(_args(n=n), FAKE, 8, -100, 0.0, FAKE * 16, 1 << 50)
         assert ei.value.status == native.E_INVALID
+
+
+def _size(k=1, **kw):
+    return native.mfsdp_head_loss_workspace_size(_args(**kw), k)
+
+
+OUTPUTS = [dict(), dict(dx=None), dict(dw=None), dict(dx=None, dw=None)]
+SIDES = [(1, 1), (128, 64), (300, 64), (1000, 64), (4000, 128), (2000, 2048), (4096, 8), (4095, 264), (5000, 130), (400, 4000),
+         (50257, 768), (128256, 4096), (128256, 4095), (128256, 32768), (1 << 20, 64), (90, 1 << 20)]
+
+
+@pytest.mark.parametrize("dtype", [native.BF16, native.F32])
+@pytest.mark.parametrize("v,h", SIDES)
+def test_fewer_tokens_never_need_more_workspace(v, h, dtype):
+    """A workspace sized for the largest batch serves every smaller one: few tokens, one pass, several passes."""
+    counts = sorted({c + d for c in (1, 32, 64, 128, 256, 384, 512, 777, 1024, 2048, 4096, 6000, 8192, 8371, 8448, 10000, 16384,
+                                     20000, 65536, 70000, 1 << 20, 1 << 25) for d in (-1, 0, 1) if 0 < c + d <= 1 << 25})
+    for outs in OUTPUTS:
+        for chunk in (0, 256, 5000):
+            last = 0
+            for n in counts:
+                now = _size(n=n, v=v, h=h, dtype=dtype, chunk_rows=chunk, **outs)
+                assert now >= last, (n, outs, chunk, last, now)
+                last = now
+
+
+@pytest.mark.parametrize("dtype", [native.BF16, native.F32])
+def test_fewer_outputs_and_slots_never_need_more_workspace_at_any_size(dtype):
+    import random
+    rng = random.Random(5)
+    log = lambda hi: int(2 ** rng.uniform(0, hi))  # noqa: E731
+    sizes = [(log(18), log(20), log(15)) for _ in range(1500)] + [(65536, 1 << 20, 64), (65536, 128256, 32768)]
+    for n, v, h in sizes:
+        kw = dict(n=n, v=v, h=h, dtype=dtype, chunk_rows=rng.choice((0, 0, 256, 4096)))
+        k = rng.randint(2, 256)
+        both = _size(k, **kw)
+        for outs in OUTPUTS[1:]:
+            some = _size(k, **kw, **outs)
+            assert some <= both, (kw, outs, some, both)
+            assert _size(k, **kw, dx=None, dw=None) <= some, (kw, outs)
+        assert _size(rng.randint(1, k), **kw) <= both
+        fewer = dict(kw, n=rng.randint(1, n))
+        assert _size(k, **fewer) <= both, (kw, fewer)
