@@ -423,7 +423,8 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  *                outputs has to be given, unless n is 0)
  *   chunk_rows   0, or the most rows of x per pass (rounded up to 256). A row of a pass takes 2 v bytes (F32: 8 v) where
  *                gradients are asked for; more than one pass takes more time, and with dw another 4 v h bytes for its sum.
- *                0: with gradients as many rows as fit 2 GiB of 16-bit logits; without, as many as take the same workspace.
+ *                0: with gradients as many rows as fit 2 GiB of 16-bit logits, or all where those beyond take less than that
+ *                sum; without, as many as take the same workspace.
  * No output may overlap an input or another output.
  * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0. The other rows
  * and w have to be finite: an infinity or a NaN there may make any result NaN. A BF16 logit that overflows to -inf is a

@@ -230,6 +230,9 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
     const int64_t slots = (kLossMaxTop - k) * 4;
     if (!p.grads)  // as many rows as take the bytes of those with gradients, with the most slots a row (the same for any k)
       p.chunk = std::min({p.n_pad, asked, std::max(with_grads, with_grads * (grad_row + slots) / (loss_row + slots) / 256 * 256)});
+    else if (a->dw && a->chunk_rows == 0 && p.n_pad <= kMaxChunk &&
+             p.n_pad * grad_row <= with_grads * grad_row + p.vp * p.hp * 4)
+      p.chunk = p.n_pad;  // one pass where the rows beyond with_grads take no more than the sum of dw over two
   }
   const int64_t groups = (p.vp + p.group - 1) / p.group;
   // many tokens: the logits' lanes (rows) store whole lines; few: a row's partials are read in one piece

@@ -215,3 +215,14 @@ def test_fewer_outputs_and_slots_never_need_more_workspace_at_any_size(dtype):
         assert _size(rng.randint(1, k), **kw) <= both
         fewer = dict(kw, n=rng.randint(1, n))
         assert _size(k, **fewer) <= both, (kw, fewer)
+
+
+def test_one_pass_where_several_would_need_more_workspace():
+    """A few rows beyond 2 GiB of logits: their logits take less than dw's sum over two passes, which is left out."""
+    kw = dict(v=128256, h=4096)
+    most = 8192
+    total = 4 * 128256 * 4096
+    assert _size(n=most + 1, **kw) - _size(n=most, **kw) < total // 10
+    assert _size(n=65536, **kw) > _size(n=65536, dw=None, **kw) + total - 1
+    # (asked for by the caller: 256 rows a pass and the sum)
+    assert _size(n=1024, chunk_rows=256, **kw) > total
