@@ -718,3 +718,73 @@ def test_teacher_logits_over_a_small_temperature(dtype):
     q[np.arange(n)[:, None], ids] = True
     _check(got, ref, x64, w64, dtype, q, inv_t=1 / temp, what=f"small temperature {dtype}")
     _check_loss(got, ref)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_both_gradients_of_a_sure_token(dtype):
+    """Small integers, exact in either type: the loss is near 0, and both gradients are sums of probabilities of e^-12 and
+    less. A probability is off by 2^-16 (bf16, no target: its 16-bit code's 2^-11 ln 2 too); an element of dz by its parts, u of
+    itself or 2^-40 of its row's largest (bf16: two parts, 2^-16, and p below 2^-64 of the label's is 0: the last token's logits
+    are e^-44 = 2^-63.5 and less); then the sum and the result's rounding."""
+    n, v, h = 6, 301, 32
+    rng = np.random.default_rng(44)
+    w = rng.integers(-1, 2, (v, h)).astype(np.float64)
+    w[:, 0] = -1
+    w[7] = 0
+    w[7, 0] = 1
+    x = np.zeros((n, h))
+    x[:, 0] = np.arange(12, 12 + 2 * n, 2)
+    x[:, 1:4] = rng.integers(-1, 2, (n, 3))
+    store = (lambda a: synth.f32_to_bf16_bits(a.astype(np.float32))) if dtype == BF16 else (lambda a: a.astype(np.float32))
+    t = np.full(n, 7)
+    got = _call("xent", store(x), store(w), dtype, t, reduction="sum")
+    r = OL.linear_xent(x, w, t, reduction="sum")
+    np.testing.assert_allclose(got["token_loss"], r.token_loss, rtol=2.0 ** -16, atol=0)
+    target = np.zeros((n, v), bool)
+    target[:, 7] = True
+    rel = 2.0 ** -16 + (2.0 ** -16 + np.where(target, 0.0, 2.0 ** -11 * np.log(2)) if dtype == BF16 else U)
+    ddz = np.abs(r.dz) * rel + (np.where(target, 0.0, 2.0 ** -64) if dtype == BF16 else 2.0 ** -40 * np.abs(r.dz).max(1)[:, None])
+    half = 2.0 ** -8 if dtype == BF16 else U
+    for name, acc, want, e, size in (("dx", v, r.dx, ddz @ np.abs(w), np.abs(r.dz) @ np.abs(w)),
+                                     ("dw", n, r.dw, ddz.T @ np.abs(x), np.abs(r.dz).T @ np.abs(x))):
+        tol = e + 2 * (acc + 8) * U * size
+        tol = tol + half * (np.abs(want) + tol) + 1e-37
+        err = np.abs(got[name] - want)
+        _say(dtype, name, "worst share of the bound:", float((err / tol).max()))
+        assert (err <= tol).all(), name
+
+
+@pytest.mark.parametrize("n,v,h", [(9, 300, 48), (300, 900, 136)])
+def test_a_head_whose_rows_differ_widely(n, v, h):
+    """fp32: rows of w from 1 down to 2^-30 of the largest, which no token holds likely, so that dx is made of the small ones. A
+    value of w is held to u of itself or 2^-40 of the largest; x and dz each relative to their rows."""
+    rng = np.random.default_rng(45)
+    x, w, x64, w64 = _inputs(rng, n, v, h, F32)
+    x64 = np.abs(x64) + 0.5
+    x = x64.astype(np.float32)
+    x64 = x.astype(np.float64)
+    size = 2.0 ** -rng.integers(1, 31, v)
+    w = (w64 * size[:, None]).astype(np.float32)
+    w[:3] = -40.0 / h ** 0.5
+    w64 = w.astype(np.float64)
+    t = rng.integers(3, v, n)
+    got = _call("xent", x, w, F32, t, reduction="sum")
+    r = OL.linear_xent(x64, w64, t, reduction="sum")
+    assert np.exp(r.z[:, :3] - r.lse[:, None]).max() < 2.0 ** -20
+    lost = 2.0 ** -40 * np.abs(w64).max()
+    dz_z = 2 * (h + 8) * U * (np.abs(x64) @ np.abs(w64).T) + lost * np.abs(x64).sum(1)[:, None]
+    dr = dz_z.max(1)
+    tol = 2 * dr + 2.0 ** -17 + 2.0 ** -18 * (np.abs(r.token_loss) + np.abs(r.z).max(1) + np.log(v))
+    assert (np.abs(got["token_loss"] - r.token_loss) <= tol).all()
+    p = np.exp(r.z - r.lse[:, None])
+    q = np.zeros((n, v), bool)
+    q[np.arange(n), t] = True
+    ddz = p * (2 * dr + 2.0 ** -16)[:, None] + np.where(q, (p + 1) * 2.0 ** -18, 2.0 ** -60)
+    ddz = ddz + U * (np.abs(r.dz) + ddz) + 2.0 ** -40 * np.abs(r.dz).max(1)[:, None]
+    for name, acc, want, e, s in (("dx", v, r.dx, ddz @ np.abs(w64) + lost * np.abs(r.dz).sum(1)[:, None], np.abs(r.dz) @ np.abs(w64)),
+                                  ("dw", n, r.dw, ddz.T @ np.abs(x64), np.abs(r.dz).T @ np.abs(x64))):
+        tol = e + 2 * (acc + 8) * U * s
+        tol = tol + U * (np.abs(want) + tol) + 1e-37
+        err = np.abs(got[name] - want)
+        _say(name, "worst share of the bound:", float((err / tol).max()))
+        assert (err <= tol).all(), name
