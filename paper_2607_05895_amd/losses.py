@@ -56,6 +56,16 @@ class _HeadLoss(torch.autograd.Function):
         return dx.view(ctx.shape) if dx is not None else None, dw, None, None
 
 
+def _weights(token_weight: Optional[torch.Tensor], shape: torch.Size) -> Optional[torch.Tensor]:
+    """One weight per token, in the tokens' own shape or as one dimension (any other of as many elements, a transposed one
+    for instance, would give tokens each other's weights)."""
+    if token_weight is None:
+        return None
+    if token_weight.shape not in (shape, (shape.numel(),)):
+        raise ValueError(f"token_weight: shape {tuple(token_weight.shape)} where {tuple(shape)} is required")
+    return _dense(token_weight.reshape(-1))
+
+
 def _check_head(hidden: torch.Tensor, weight: torch.Tensor) -> None:
     if not hidden.is_cuda or not weight.is_cuda:
         raise ValueError(f"the losses run on the GPU only; got {hidden.device} and {weight.device} tensors")
@@ -68,12 +78,11 @@ def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: to
                          scale: float = 1.0, chunk_rows: int = 0) -> torch.Tensor:
     """Softmax cross entropy of hidden @ weight.T with the labels `targets` (hidden's shape without its last dimension):
     scale / D sum_r a_r (lse_r - z_{r, t_r} + z_loss lse_r^2), D = 1 ("sum") or the sum of the a_r of the labelled
-    tokens ("mean"). token_weight: a_r (float32; no gradient). A call with all labels ignored gives 0."""
+    tokens ("mean"). token_weight: a_r (targets' shape, float32; no gradient). A call with all labels ignored gives 0."""
     _check_head(hidden, weight)
     if targets.shape != hidden.shape[:-1]:
         raise ValueError(f"targets: shape {tuple(targets.shape)} where {tuple(hidden.shape[:-1])} is required")
-    t = _dense(targets.reshape(-1))
-    a = None if token_weight is None else _dense(token_weight.reshape(-1))
+    t, a = _dense(targets.reshape(-1)), _weights(token_weight, targets.shape)
 
     def call(x, w, **out):
         native.linear_xent_t(x, w, t, ignore_index=ignore_index, reduction=reduction, scale=scale, token_weight=a,
@@ -94,7 +103,7 @@ def linear_distillation(hidden: torch.Tensor, weight: torch.Tensor, top_ids: tor
         if t.shape != want:
             raise ValueError(f"{what}: shape {tuple(t.shape)} where {want} is required")
     ids, logits = _rows(top_ids, 1, "top_ids"), _rows(top_logits, 1, "top_logits")
-    a = None if token_weight is None else _dense(token_weight.reshape(-1))
+    a = _weights(token_weight, hidden.shape[:-1])
 
     def call(x, w, **out):
         native.linear_distill_t(x, w, ids, logits, temperature=temperature, reduction=reduction, scale=scale,

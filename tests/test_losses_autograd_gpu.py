@@ -201,3 +201,20 @@ def test_shifted_views(dtype):
     want = grads(losses.linear_distillation(hid[1:].clone(), w[1:].clone(), top[1:].clone(), lg[1:].clone()))
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert torch.equal(losses.token_losses(hid[:-1], w, ids[1:]), losses.token_losses(hid[:-1].clone(), w, ids[1:].clone()))
+
+
+def test_token_weights_of_another_shape_are_refused():
+    """As many weights in another order of dimensions belong to other tokens; the tokens' shape and one dimension do not."""
+    import torch
+    from paper_2607_05895_amd import losses
+    B, T, v, h = 2, 3, 40, 16
+    x, w = torch.randn(B, T, h, device="cuda"), torch.randn(v, h, device="cuda")
+    t, ids, lg = (torch.randint(0, v, s, device="cuda") for s in ((B, T), (B, T, 2), (B, T, 2)))
+    a = torch.rand(B, T, device="cuda")
+    calls = (lambda a: losses.linear_cross_entropy(x, w, t, token_weight=a, reduction="sum"),
+             lambda a: losses.linear_distillation(x, w, ids, lg.float(), token_weight=a, reduction="sum"))
+    for call in calls:
+        assert float(call(a)) == float(call(a.reshape(-1)))
+        for bad in (a.t(), a[:, :2], a[None], a[:1], a.reshape(1, -1), a[0, 0]):
+            with pytest.raises(ValueError, match="token_weight"):
+                call(bad)
