@@ -68,8 +68,16 @@ struct Plan {
   size_t bytes = 0;
 };
 
-// The most tokens, and the fewest ids, of the products for a few tokens.
-constexpr int64_t kStreamTokens = 128, kStreamIds = 4096;
+// The products for a few tokens: at most kStreamTokens, on at least stream_ids(tokens) ids. Measured in us, tiles' kernels
+// against these, loss alone and with both gradients:
+//   1 token    4096 x 768: 22, 21 and 44, 36      16384 x 2048: 39, 31 and 109, 73      128256 x 4096: 242, 230 and 1034, 615
+//   64 tokens  4096 x 768: 23, 21 and 47, 44      16384 x 2048: 41, 36 and 118, 86      128256 x 4096: 244, 241 and 1053, 654
+//   128        8192 x 768: 23, 29 and 60, 62      16384 x 2048: 41, 51 and 126, 119     128256 x 4096: 246, 285 and 1257, 963
+//              4096 x 4096: 38, 77 and 100, 121   32768 x 4096: 78, 95 and 343, 268     50257 x 768: 41, 37 and 152, 125
+// (512 to 2048 ids: the same time up to 32 tokens. Beyond 64 tokens a wave multiplies twice as much per byte of w, which a
+// loss alone has nothing to make up for: it stays up to 1.5 times slower below some 40000 ids.)
+constexpr int64_t kStreamTokens = 128;
+constexpr int64_t stream_ids(int64_t tokens) { return tokens <= 64 ? 4096 : 12288; }
 
 constexpr int64_t kMinRange = 16, kMaxRanges = 64;        // K steps of a range at least; ranges of dx at most
 constexpr int64_t kMaxItems = 512;                        // tiles of the logits in K ranges at most
@@ -217,8 +225,8 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   const int64_t loss_row = p.hp * es + p.vp / kLossGroup * 8 + k * 4 + 16;
   const int64_t grad_row = loss_row + p.vp * 2 * (p.f32 ? 2 : 1) + (p.f32 ? p.vp * 4 + 5 : 0);
   int64_t with_grads = 0;  // rows of a pass
-  const bool streams = !p.copy && p.v >= kStreamIds;  // where the tokens are few
-  if (streams && p.n > 0 && p.n <= kStreamTokens) {
+  auto streams = [&](int64_t tokens) { return !p.copy && p.v >= stream_ids(tokens); };
+  if (p.n > 0 && p.n <= kStreamTokens && streams(p.n)) {
     p.stream = p.n <= 32 ? 1 : p.n <= 64 ? 2 : 4;
     p.group = 32;
     p.chunk = p.n_pad = 32 * p.stream;
@@ -258,7 +266,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
       choose_grads(rows, p.v, p.h, p.out_nseg * vsteps, a->dw ? wsteps : 0, room, p.dx, p.dw);
       p.dx.nk = int(vsteps);
       part = std::max(part, room);
-      if (streams) part = std::max(part, stream_ranges(p, 4) * kStreamTokens * p.hp * 4);  // a call over few tokens
+      if (streams(1)) part = std::max(part, stream_ranges(p, 4) * kStreamTokens * p.hp * 4);  // a call over few tokens
     }
   }
   if (a->dw && (p.stream || !a->dx)) p.dw = choose(p.v, p.h, wsteps, false);
@@ -288,7 +296,7 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
   if (p.copy) p.wb = take(p.v * p.ldw * es);
   if (p.grads) {
     // (up to 128 tokens on the tiles' kernels: two parts of 256 rows, which 129 tokens keep room for)
-    p.codes = take(std::max(p.chunk * p.dz_parts, streams || p.f32 ? 0 : int64_t(512)) * p.vp * 2);
+    p.codes = take(std::max(p.chunk * p.dz_parts, streams(kStreamTokens) || p.f32 ? 0 : int64_t(512)) * p.vp * 2);
     if (p.f32) {
       p.z32 = take(p.chunk * p.vp * 4);
       p.row_most = take(p.chunk * 4);

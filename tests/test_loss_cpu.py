@@ -179,7 +179,7 @@ def _size(k=1, **kw):
 
 
 OUTPUTS = [dict(), dict(dx=None), dict(dw=None), dict(dx=None, dw=None)]
-SIDES = [(1, 1), (128, 64), (300, 64), (1000, 64), (4000, 128), (2000, 2048), (4096, 8), (4095, 264), (5000, 130), (400, 4000),
+SIDES = [(1, 1), (128, 64), (300, 64), (1000, 64), (4000, 128), (2000, 2048), (4096, 8), (4095, 264), (12287, 264), (12288, 264), (9001, 8192), (5000, 130), (400, 4000),
          (50257, 768), (128256, 4096), (128256, 4095), (128256, 32768), (1 << 20, 64), (90, 1 << 20)]
 
 

@@ -788,3 +788,25 @@ def test_a_head_whose_rows_differ_widely(n, v, h):
         err = np.abs(got[name] - want)
         _say(name, "worst share of the bound:", float((err / tol).max()))
         assert (err <= tol).all(), name
+
+
+@pytest.mark.parametrize("n,v,h,k", [(64, 12289, 264, 1), (65, 12287, 264, 1), (65, 12288, 72, 1), (100, 13001, 136, 5), (128, 12300, 320, 33),
+                                     (129, 12288, 72, 3), (128, 16384, 1000, 1)])
+def test_around_the_limits_of_a_few_tokens(n, v, h, k):
+    rng = np.random.default_rng(46)
+    x, w, x64, w64 = _inputs(rng, n, v, h, BF16)
+    _say(n, v, h, k)
+    q = np.zeros((n, v), bool)
+    if k == 1:
+        t = _labels(rng, n, v)
+        got = _call("xent", x, w, BF16, t, z_loss=1e-3)
+        ref = _Ref(OL.linear_xent(x64, w64, t, z_loss=1e-3), t >= 0, None, "mean", 1.0)
+        q[np.nonzero(t >= 0)[0], t[t >= 0]] = True
+        _check(got, ref, x64, w64, BF16, q, z_loss=1e-3, what=f"limits {n}x{v}x{h}")
+    else:
+        ids, lg = _teacher(rng, n, v, k)
+        got = _call("distill", x, w, BF16, (ids, lg, F32), temperature=1.5)
+        ref = _Ref(OL.linear_distill(x64, w64, ids, lg, temperature=1.5), (ids >= 0).any(1), None, "mean", 1.0)
+        q[np.repeat(np.arange(n), k).reshape(n, k)[ids >= 0], ids[ids >= 0]] = True
+        _check(got, ref, x64, w64, BF16, q, inv_t=1 / 1.5, what=f"limits {n}x{v}x{h},{k}")
+    _check_loss(got, ref)
