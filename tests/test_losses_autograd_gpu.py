@@ -218,3 +218,42 @@ def test_token_weights_of_another_shape_are_refused():
         for bad in (a.t(), a[:, :2], a[None], a[:1], a.reshape(1, -1), a[0, 0]):
             with pytest.raises(ValueError, match="token_weight"):
                 call(bad)
+
+
+@pytest.mark.parametrize("dtype", [synth.BF16, synth.F32])
+def test_captured_forward_and_backward(dtype):
+    """Both losses and their gradients in one graph, replayed on new inputs with eager work in between: the eager bits."""
+    import torch
+    from paper_2607_05895_amd import losses
+    rng = np.random.default_rng(6)
+    n, v, h = 70, 900, 72
+    xs = [to_dev(_store(rng.standard_normal((n, h)), dtype)[0], dtype) for _ in range(2)]
+    w = _leaf(_store(rng.standard_normal((v, h)) / 8, dtype)[0], dtype)
+    t = torch.from_numpy(rng.integers(0, v, n)).cuda()
+    ids, lg = torch.from_numpy(rng.integers(0, v, (n, 4))).cuda(), torch.randn(n, 4, device="cuda")
+    x = xs[0].clone().requires_grad_(True)
+
+    def step():
+        loss = 0.75 * losses.linear_cross_entropy(x, w, t) + losses.linear_distillation(x, w, ids, lg, temperature=2.0)
+        return [loss.detach().clone(), *torch.autograd.grad(loss, (x, w))]
+
+    want = []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in (0, 1):
+            with torch.no_grad():
+                x.copy_(xs[i])
+            want.append([a.clone() for a in step()])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for i in (0, 1, 0):
+        with torch.no_grad():
+            x.copy_(xs[i])
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[i])), i
+        losses.token_losses(xs[1], w, t)
+        torch.cuda.synchronize()
