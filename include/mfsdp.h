@@ -429,11 +429,15 @@ typedef enum { MFSDP_SUM = 0, MFSDP_MEAN = 1 } mfsdp_reduction;
  * A row of x whose token does not count is not looked at (it may hold anything) and its dx is 0. The other rows
  * and w have to be finite: an infinity or a NaN there may make any result NaN. A BF16 logit that overflows to -inf is a
  * probability of 0.
- * Precision: bf16 products have fp32 accumulation; the softmax is formed in fp32, the sum of a row without its largest
- * term, so that the loss of a token that the model is sure of keeps its digits; the logits' gradient is rounded to bf16
- * before its two products (up to 128 tokens it is held to 16 bits and more), and each result once to bf16. F32: products at fp32 accuracy (two scaled fp16 parts per operand:
- * a value of w is off by at most 2^-24 of itself or 2^-40 of w's largest, an element of a row of x or of the logits' gradient by as
- * much relative to its row), everything else in fp32. */
+ * Precision of the losses: products with fp32 accumulation, the softmax in fp32, the sum of a row without its largest term,
+ * so that the loss of a token that the model is sure of keeps its digits.
+ * Gradients, BF16: the probability of an id that is no target comes from a 16-bit logit, for any number of tokens: off by up
+ * to 3.4e-4 of itself, and 0 below 2^-64 of the largest of its 32 or 64 neighbours; a target's comes from the fp32 logit. The
+ * logits' gradient is rounded to bf16 (2^-8 of itself) before its two products; up to 128 tokens it goes into them in two bf16
+ * parts (2^-16). Each result is rounded once to bf16.
+ * F32: products at fp32 accuracy from two scaled fp16 parts per operand: a value of w is off by at most 2^-24 of itself or 2^-40
+ * of w's largest (so values below 2^-16 of the largest lose digits), an element of a row of x or of the logits' gradient by as
+ * much relative to its row. Everything else is in fp32. */
 typedef struct {
   const void* x;
   const void* w;

@@ -1055,7 +1055,7 @@ __device__ __forceinline__ float target_pq(float q, float d, float e, float s) {
 }
 
 // RPB rows per workgroup of 1024: thread t goes through groups t / RPB, + 1024 / RPB, ... of row t % RPB. Many tokens: 32
-// rows, whose partials of a group lie together. Few: one row, whose partials lie in one piece (128256 ids, 48 tokens: 7 us;
+// rows, whose partials of a group lie together. Few: one row, whose partials lie in one piece (128256 ids, 48 tokens: 9 us;
 // with four rows each and the other layout 19.5, when a workgroup reads four times the bytes it needs).
 template <int RPB>
 __global__ __launch_bounds__(1024) void loss_rows_kernel(const LossRows a) {
@@ -1366,7 +1366,8 @@ __global__ __launch_bounds__(256) void loss_join_kernel(const LossJoin a) {
 // ahead by direct loads. Bound by HBM: w is read once, QB bytes per step, with up to (NST - 1) steps of it in flight per CU.
 // logits: a stage holds QR rows of w by KT of h; a wave takes all tokens by 32 rows of w, and half of the step's K where
 //   QR = 128 (the halves are added in LDS at the tile's end); chunk c of row r in slot c ^ r % 16 (KT = 64: c ^ r / 2 % 8). 128
-//   rows of 256 bytes rather than 256 of 128: a head of 128256 x 4096 is read in 215 us (4.9 TB/s) instead of 227; more
+//   rows of 256 bytes rather than 256 of 128: a head of 128256 x 4096 is read in 223 us on average (4.7 TB/s; 212 at best),
+//   and a call of one token takes 230 us instead of 243, of 48 tokens 240 instead of 255 (50257 x 768: 28.5 and 26.5); more
 //   tokens leave no room for it.
 // dx: KT rows of w by 256 of h, a wave 32 columns; chunk c of row r in slot c ^ 2 (r % 4); fragments read transposed.
 // Past a row's end lie the next row's values, past w's end its last ones: they meet zeros of x or dz, or belong to columns
@@ -1598,7 +1599,7 @@ __global__ __launch_bounds__(512, 1) void loss_stream_kernel(const LossStream a)
 // dw of at most 32 KS tokens: K is a few steps, and writing dw all there is to it (HBM). A workgroup of four waves keeps CT
 // columns of x in registers and goes through blocks of 64 rows (ids), gridDim.y blocks apart: both parts of the next block of
 // dz are on their way while this one's product goes out, through LDS, so that a wave stores whole rows of CT columns. (48
-// tokens, 128256 x 4096, 1.05 GB: 234 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel
+// tokens, 128256 x 4096, 1.05 GB: 240 us; one block per workgroup, x read again for each: 327; the persistent tiles' kernel
 // more.) Non-temporal stores: with plain ones it takes 245 us, and what reads w after it 284 us instead of 233, waiting for
 // the caches to write dw back (the whole call 728 -> 670 us).
 template <int KS>

@@ -565,7 +565,7 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (!last) mw.part = f32p(p.acc);
     }
     LossGemm2 both{};
-    // dw of a few tokens on a kernel of its own (48 tokens, 128256 x 4096: 247 us, 295 on the tiles' kernel), unless its
+    // dw of a few tokens on a kernel of its own (48 tokens, 128256 x 4096, dx and dw: 654 us, 865 with dw on the tiles' kernel; 100 tokens: 931 and 1073), unless its
     // tiles go into dx's launch in one round (64 tokens, 1000 x 64, dx and dw: 13 us in one launch, 20 in two)
     const bool short_dw = !p.f32 && first && last && rows <= kStreamTokens && (p.stream || !a->dx || p.dw.items() > 256);
     // otherwise one launch where both use the same tile, the longer tiles first

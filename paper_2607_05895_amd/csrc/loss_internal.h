@@ -9,14 +9,14 @@
 // largest value to [2^14, 2^15): 22 bits and the second part's sign, so a value is off by at most 2^-24 of itself, as in
 // fp32, down to 2^-16 of the largest, and by 2^-40 of the largest below that. A product runs over three pairs of parts, one K
 // segment each; the fourth would add at most 2^-24 of each product. (Three bf16 parts need no scale, and six pairs: 1024
-// tokens on a 50257 x 768 head, both gradients, 1490 us; so 925.) The scale is one for all of w, and one per row of x and of
+// tokens on a 50257 x 768 head, both gradients, 1490 us; so 926.) The scale is one for all of w, and one per row of x and of
 // dz, so that no token's digits depend on another token. For dw, which sums over the tokens, x is split a second time, its
 // rows divided by dz's scales. Values that are not finite are left out of the scales.
 //
 // dz of bf16 inputs is rounded to bf16. Up to 128 tokens it is held in two bf16 parts instead (its products run over both,
 // one K segment each): there one rounding of a target's dz is a share of a whole row of dx and dw that no other token evens
 // out (up to 2^-8, beside the results' own rounding), and the second part costs next to nothing where reading w and writing
-// dw take the time (48 tokens, 128256 x 4096: 722 us in one part, 727 in two).
+// dw take the time (48 tokens, 128256 x 4096, before dw's stores went past the caches: 722 us in one part, 727 in two).
 //
 // Between the logits and their gradient a chunk of bf16 inputs holds each logit in 16 bits: the distance
 // from the largest of its row in its 64 columns, in steps of 64 / 65535 of a factor of two. That is a relative error of p of
