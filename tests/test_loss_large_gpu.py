@@ -139,3 +139,25 @@ def test_one_pass_beyond_2_gib_of_logits():
     x, w, t = _inputs(n, v, h, torch.bfloat16, 7)
     print(n, v, h, flush=True)
     _compare("xent", _run("xent", x, w, t, ("dx", "dw"), 1.0, 0), x, w, t)
+
+
+@pytest.mark.parametrize("n,v,h", [(18000, 1 << 20, 64), (9000, 128256, 1032)])
+def test_a_loss_alone_over_many_rows(n, v, h):
+    """More rows than one pass with gradients takes (the first: than one without, too): tokens of every pass, and of their ends,
+    against 64 bits; the same tokens alone; the reduced loss against their sum."""
+    import torch
+    x, w, t = _inputs(n, v, h, torch.bfloat16, 9)
+    print(n, v, h, flush=True)
+    got = _run("xent", x, w, t, (), 1.0, 0)
+    rows = torch.unique(torch.cat([torch.arange(0, n, n // 90, device="cuda"), torch.arange(n - 8, n, device="cuda")] +
+                                  [torch.arange(c - 3, c + 3, device="cuda") for c in (1024, 8192, 16384, 17152) if c + 3 < n]))
+    xr, tr = x[rows], t[rows]
+    z = xr.double() @ w.double().T
+    lse = torch.logsumexp(z, 1)
+    on = tr >= 0
+    want = torch.where(on, lse - z.gather(1, tr.clamp(min=0)[:, None])[:, 0], 0.0)
+    dr = (xr.double().abs() @ w.double().abs().T).amax(1) * (2 * (h + 8) * U)
+    tol = 2 * dr + 2.0 ** -17 + 2.0 ** -18 * (want.abs() + (z.amax(1) - z.amin(1)) + float(np.log(v)))
+    assert bool(((got["token_loss"][rows].double() - want).abs() <= torch.where(on, tol, 0.0)).all())
+    sums = got["token_loss"].double().sum() / (t >= 0).sum()
+    assert bool(torch.isfinite(got["token_loss"]).all()) and abs(float(got["loss"]) - float(sums)) <= 2.0 ** -20 * float(sums)
