@@ -74,8 +74,9 @@ struct Plan {
 //   64 tokens  4096 x 768: 23, 21 and 47, 44      16384 x 2048: 41, 36 and 118, 86      128256 x 4096: 244, 241 and 1053, 654
 //   128        8192 x 768: 23, 29 and 60, 62      16384 x 2048: 41, 51 and 126, 119     128256 x 4096: 246, 285 and 1257, 963
 //              4096 x 4096: 38, 77 and 100, 121   32768 x 4096: 78, 95 and 343, 268     50257 x 768: 41, 37 and 152, 125
-// (512 to 2048 ids: the same time up to 32 tokens. Beyond 64 tokens a wave multiplies twice as much per byte of w, which a
-// loss alone has nothing to make up for: it stays up to 1.5 times slower below some 40000 ids.)
+// (512 to 2048 ids: the same time up to 32 tokens. 4096 x 8192 is too short a head: 1 token 44, 59 and 110, 94. Beyond 64 tokens
+// a wave multiplies twice as much per byte of w, which a loss alone has nothing to make up for: it is up to 1.5 times slower
+// below some 40000 ids.)
 constexpr int64_t kStreamTokens = 128;
 constexpr int64_t stream_ids(int64_t tokens) { return tokens <= 64 ? 4096 : 12288; }
 
@@ -120,7 +121,8 @@ Gemm choose(int64_t M, int64_t N, int64_t steps, bool ranges) {
   double us = 0.0;
   for (int tile : {kLossTile, kLossTileSmall}) {
     Gemm g = grid_of(tile, M, N);
-    const int64_t tiles = g.items(), most = ranges && tile == kLossTileSmall ? std::min<int64_t>(kMaxItems / tiles, steps / kMinRange) : 1;
+    const int64_t tiles = g.items();
+    const int64_t most = ranges && tile == kLossTileSmall ? std::min(kMaxItems / tiles, steps / kMinRange) : 1;
     for (int64_t s = 1; s == 1 || s <= most; ++s) {
       const int64_t kper = s == 1 ? steps : up((steps + s - 1) / s, 2), items = tiles * s;
       if (s > 1 && (steps + kper - 1) / kper != s) continue;
@@ -235,9 +237,9 @@ Plan make_plan(const mfsdp_head_loss* a, int64_t k) {
     const int64_t asked = a->chunk_rows > 0 ? std::min(kMaxChunk, up(a->chunk_rows, 256)) : kMaxChunk;
     with_grads = std::min({p.n_pad, asked, std::max<int64_t>(256, kLogitBytes / (2 * p.vp) / 256 * 256)});
     p.chunk = with_grads;
-    const int64_t slots = (kLossMaxTop - k) * 4;
+    const int64_t slots = (kLossMaxTop - k) * 4, without = with_grads * (grad_row + slots) / (loss_row + slots) / 256 * 256;
     if (!p.grads)  // as many rows as take the bytes of those with gradients, with the most slots a row (the same for any k)
-      p.chunk = std::min({p.n_pad, asked, std::max(with_grads, with_grads * (grad_row + slots) / (loss_row + slots) / 256 * 256)});
+      p.chunk = std::min({p.n_pad, asked, std::max(with_grads, without)});
     else if (a->dw && a->chunk_rows == 0 && p.n_pad <= kMaxChunk &&
              p.n_pad * grad_row <= with_grads * grad_row + p.vp * p.hp * 4)
       p.chunk = p.n_pad;  // one pass where the rows beyond with_grads take no more than the sum of dw over two
@@ -565,8 +567,9 @@ int run(const mfsdp_head_loss* a, int64_t k, const Labels& l, void* workspace, s
       if (!last) mw.part = f32p(p.acc);
     }
     LossGemm2 both{};
-    // dw of a few tokens on a kernel of its own (48 tokens, 128256 x 4096, dx and dw: 654 us, 865 with dw on the tiles' kernel; 100 tokens: 931 and 1073), unless its
-    // tiles go into dx's launch in one round (64 tokens, 1000 x 64, dx and dw: 13 us in one launch, 20 in two)
+    // dw of a few tokens on a kernel of its own (128256 x 4096, the whole call with dx and dw: 48 tokens 654 us, 865 with dw on
+    // the tiles' kernel, 100 tokens 931 and 1073), unless its tiles go into dx's launch in one round (64 tokens, 1000 x 64, dx
+    // and dw: 13 us in one launch, 20 in two)
     const bool short_dw = !p.f32 && first && last && rows <= kStreamTokens && (p.stream || !a->dx || p.dw.items() > 256);
     // otherwise one launch where both use the same tile, the longer tiles first
     const bool together = a->dx && a->dw && !p.stream && !short_dw && p.dx.tile == p.dw.tile;

@@ -143,8 +143,7 @@ struct LossMaxima {
 
 // The first launch: the labels in one form (per token k different ids with weights q that add up to 1, -1 and 0 for none; the
 // sum of q log q; on: whether the token counts, 1, 0, or NaN for an id outside the vocabulary or a teacher logit of +inf or
-// NaN), the packed operands, and the
-// counters of the chunk's products set to 0.
+// NaN), the packed operands, and the counters of the chunk's products set to 0.
 struct LossPrep {
   LossLabels l;
   int64_t n_pad;

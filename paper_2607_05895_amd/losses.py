@@ -4,8 +4,8 @@
 both float32, and return the scalar loss, on torch's current stream. The logits are never held as a whole, so the
 forward pass computes the gradients as well where they are wanted (the backward pass multiplies them by the incoming
 gradient, in place, and hands them out: it can run once). That factor rounds bfloat16 gradients a second time unless it is a
-power of two; a factor that is known beforehand is better given as `scale`. `token_losses` is the loss of every token, without gradients.
-These functions only marshal arguments: the arithmetic runs in libmfsdp.so, and there is no CPU path.
+power of two; a factor that is known beforehand is better given as `scale`. `token_losses` is the loss of every token,
+without gradients. These functions only marshal arguments: the arithmetic runs in libmfsdp.so, and there is no CPU path.
 
 Forward and backward passes can be captured into a graph. As with any torch function, let no loss of an eager pass over the
 same leaves live on while their backward pass is captured: torch ties a leaf's gradient to the stream of the pass that it first
